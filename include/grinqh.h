@@ -275,6 +275,122 @@ GRINQH_API int grinqh_vmm_lut_threshold(const grinqh_layer_desc* desc, const voi
                                         const float* thresholds, uint8_t* level_map_out, float* y,
                                         int32_t flags, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The key/value cache and the attention that reads it: what a decoder layer
+ * does between its qkv and o projections.  Not part of the paper's method;
+ * conventions (device memory, streams, validation, errors) as above.
+ *
+ * Cache layout.  K and V each have one array of pages.  A page holds `page`
+ * consecutive tokens of one sequence, for every kv head:
+ *   values [n_pages][heads][page][head_dim]  in the format's type
+ *   scales [n_pages][heads][page]            fp32, GRINQH_KV_I8 only
+ * GRINQH_KV_I8 holds a head of a token as int8 codes and one scale, the value
+ * being code * scale (fp32).  With a = max|x| over the head_dim values of the
+ * row in fp32: scale = fp32(a / 127), r = fp32(127 / a), code = rne(fp32(x * r)).
+ * A row with a < 2^-100 is stored as zeros with scale 0; a row with a NaN or
+ * an infinity as zeros with a NaN scale, so whatever reads it is NaN.
+ *
+ * A batch is B sequences.  Row i of the n = row_offsets[b+1] - row_offsets[b]
+ * rows of sequence b stands at position seq_lens[b] - n + i: the rows are the
+ * last n tokens of the sequence (seq_lens counts them).  Token t of sequence b
+ * is in place t % page of page block_table[b][t / page].
+ * The batch's arrays live on the device and are read by the kernels, so a
+ * captured graph follows what later steps write there.  What the host cannot
+ * check is bounded in the kernels: offsets are clamped to 0..rows and to
+ * ascending order, lengths to 0..min(table_width * page, 2^30); rows of no
+ * sequence are not touched; memory of a page id outside 0..n_pages-1 is never accessed. */
+enum { GRINQH_F16 = 0, GRINQH_BF16 = 1, GRINQH_F32 = 2 };            /* types of dense rows */
+enum { GRINQH_KV_F16 = 0, GRINQH_KV_BF16 = 1, GRINQH_KV_I8 = 2 };    /* formats of the cache */
+
+typedef struct {
+  int32_t format;    /* GRINQH_KV_* */
+  int32_t heads;     /* kv heads, 1..1024 */
+  int32_t head_dim;  /* 64 or 128 */
+  int32_t page;      /* tokens per page, a power of two, 1..2^20 */
+  int32_t n_pages;   /* pages of the arrays, >= 1 */
+} grinqh_kv_desc;
+
+typedef struct {
+  void* k;           /* device, 16-byte aligned */
+  void* v;
+  float* k_scale;    /* device, 4-byte aligned; NULL for 16-bit formats */
+  float* v_scale;
+} grinqh_kv_cache;
+
+typedef struct {
+  const int32_t* block_table;  /* device [B][table_width]: page ids */
+  const int32_t* seq_lens;     /* device [B]: tokens of each sequence, its rows included */
+  const int32_t* row_offsets;  /* device [B + 1]: where each sequence's rows start */
+  int32_t B;                   /* sequences, 0..65535 */
+  int32_t table_width;         /* page ids per sequence, >= 1 */
+  int32_t rows;                /* rows of the dense arrays, 0..2^24 */
+} grinqh_kv_batch;
+
+/* Dense rows [rows][heads][head_dim]: the last axis contiguous, the others with
+ * strides in elements, >= 0 and multiples of 16 bytes; base 16-byte aligned.
+ * Rows that are written must not overlap. */
+typedef struct {
+  void* data;
+  int64_t row_stride;
+  int64_t head_stride;
+} grinqh_rows;
+
+/* Sizes of the arrays of K (those of V are the same): value bytes and scale
+ * bytes (0 for 16-bit formats).  Host only. */
+GRINQH_API int grinqh_kv_bytes(const grinqh_kv_desc* desc, size_t* value_bytes, size_t* scale_bytes);
+
+/* Write the batch's rows of K and V (type GRINQH_F16, GRINQH_BF16 or
+ * GRINQH_F32) into the cache, quantised as the format asks; 16-bit formats
+ * round to nearest even.  A row is not written if its position is negative or
+ * its page id out of range.  Where two rows share a slot either may stay. */
+GRINQH_API int grinqh_kv_write(const grinqh_kv_desc* desc, const grinqh_kv_cache* cache,
+                               const grinqh_kv_batch* batch, int type, const grinqh_rows* k,
+                               const grinqh_rows* v, void* stream);
+
+/* Read the batch's rows back from the cache as dense K and V of `type`
+ * (rounded to nearest even; offsets = the running sum of seq_lens reads whole
+ * sequences).  A row whose position is negative is zeros, one whose page id is
+ * out of range NaN. */
+GRINQH_API int grinqh_kv_read(const grinqh_kv_desc* desc, const grinqh_kv_cache* cache,
+                              const grinqh_kv_batch* batch, int type, const grinqh_rows* k,
+                              const grinqh_rows* v, void* stream);
+
+typedef struct {
+  int32_t heads;     /* query heads, a multiple of the cache's; kv head h serves query heads
+                        h * heads / kv_heads onwards */
+  int32_t type;      /* of q and out: GRINQH_F16 or GRINQH_BF16; a 16-bit cache has the same */
+  float scale;       /* of the scores; positive and finite (usually head_dim^-1/2) */
+  int32_t window;    /* 0: every earlier token is visible; W > 0: the row's own and the W - 1
+                        tokens before it */
+  int32_t sinks;     /* first tokens of a sequence that stay visible behind the window */
+  int32_t max_rows;  /* upper estimates of the rows and of the length of one sequence: they
+                        shape the launch and never change what is computed */
+  int32_t max_len;
+} grinqh_attend_desc;
+
+/* Attention of the batch's rows over the cache.  The row at position p sees
+ * token t iff t <= p and (window = 0 or t > p - window or t < sinks), with
+ *   s_t = scale * (q . k_t), m = max s_t, o = sum_t exp(s_t - m) v_t / sum_t exp(s_t - m)
+ * over the visible t.  A row that sees nothing (or only scores of -inf) is 0.
+ * lse (fp32 [rows][heads], contiguous, or NULL) gets m + log sum_t exp(s_t - m),
+ * -inf for such a row.  What a row does not see never reaches it, infinities
+ * and NaN included; a visible token whose page id is out of range makes the
+ * row NaN, pages that no row sees may have any id.
+ * Precision: scores, statistics and sums in fp32; exp(s_t - m), at an 8-bit
+ * cache times the value's scale, is rounded to 16 bits for the product with
+ * the values (fp16, for a bf16 cache bf16).
+ * The rows' own tokens have to be in the cache already (grinqh_kv_write).
+ * workspace: device, 16-byte aligned, of at least the size that
+ * grinqh_attend_workspace_bytes gives for the same arguments (host only; may
+ * be 0: NULL).  It holds partial results of sequences that are split over
+ * workgroups; calls on different streams need workspaces of their own. */
+GRINQH_API int grinqh_attend_workspace_bytes(const grinqh_kv_desc* desc, const grinqh_attend_desc* attend,
+                                             int32_t B, int32_t rows, size_t* bytes);
+GRINQH_API int grinqh_attend(const grinqh_kv_desc* desc, const grinqh_kv_cache* cache,
+                             const grinqh_kv_batch* batch, const grinqh_attend_desc* attend,
+                             const grinqh_rows* q, const grinqh_rows* out, float* lse,
+                             void* workspace, size_t ws_bytes, void* stream);
+
 /* Infrastructure for tests and measurements, not an operation of the paper:
  * process-wide overrides of launch choices that never change results beyond
  * rounding order.  Value 0 restores each launcher's own choice.

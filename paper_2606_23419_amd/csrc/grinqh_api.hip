@@ -25,7 +25,7 @@ int check_launch(const char* what) {
   return GRINQH_OK;
 }
 
-static void clear_error() { g_err[0] = '\0'; }
+void clear_error() { g_err[0] = '\0'; }
 
 static Options g_opt = {};
 

@@ -85,6 +85,7 @@ int option(int Options::*field);
 
 // Error reporting (per thread), defined in grinqh_api.hip.
 int fail(int status, const char* fmt, ...);
+void clear_error();
 int check_launch(const char* what);
 
 // Compute units of the current device (prefill.hip).

@@ -9,6 +9,7 @@ load, importing this module raises.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -30,6 +31,12 @@ GRINQH_OPT_GROUPS_PER_WG = 2
 GRINQH_OPT_PREFILL_TILE = 3
 GRINQH_OPT_LUT_GROUPS = 4
 GRINQH_OPT_PREFILL_CUS = 5
+GRINQH_F16 = 0
+GRINQH_BF16 = 1
+GRINQH_F32 = 2
+GRINQH_KV_F16 = 0
+GRINQH_KV_BF16 = 1
+GRINQH_KV_I8 = 2
 GRINQH_KERNEL_AUTO = 0
 GRINQH_KERNEL_PER_PLANE = 1
 GRINQH_KERNEL_GENERAL = 2
@@ -40,7 +47,8 @@ EXPORTED = (
     "grinqh_workspace_bytes", "grinqh_calibrate", "grinqh_assign", "grinqh_vmm",
     "grinqh_vmm_threshold", "grinqh_prefill", "grinqh_lut_entries", "grinqh_vmm_lut",
     "grinqh_vmm_lut_threshold", "grinqh_set_option", "grinqh_calibrate_noalloc",
-    "grinqh_stream_read", "grinqh_vmm_topk", "grinqh_last_error",
+    "grinqh_stream_read", "grinqh_vmm_topk", "grinqh_last_error", "grinqh_kv_bytes",
+    "grinqh_kv_write", "grinqh_kv_read", "grinqh_attend_workspace_bytes", "grinqh_attend",
 )
 
 
@@ -64,6 +72,37 @@ class LayerDesc(ctypes.Structure):
     def __repr__(self):
         return (f"LayerDesc(K={self.K}, N={self.N}, levels={self.levels()}, "
                 f"plane_bits={self.plane_bits}, tile_n={self.tile_n})")
+
+
+class KvDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("format", "heads", "head_dim", "page", "n_pages")]
+
+    def __repr__(self):
+        return "KvDesc(" + ", ".join(f"{n}={getattr(self, n)}" for n, _ in self._fields_) + ")"
+
+
+class AttendDesc(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("type", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("max_len", ctypes.c_int32)]
+
+
+class _KvCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class _KvBatch(ctypes.Structure):
+    _fields_ = [("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("row_offsets", ctypes.c_void_p),
+                ("B", ctypes.c_int32), ("table_width", ctypes.c_int32), ("rows", ctypes.c_int32)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+# The arrays of a cache and of a batch, as grinqh.h lays them out.
+KvCache = collections.namedtuple("KvCache", "k v k_scale v_scale")
+KvBatch = collections.namedtuple("KvBatch", "block_table seq_lens row_offsets")
 
 
 def _load():
@@ -92,6 +131,15 @@ def _load():
         "grinqh_set_option": [ctypes.c_int, ctypes.c_int],
         "grinqh_calibrate_noalloc": [dp, vp, i32, ctypes.POINTER(i32), vp, vp],
         "grinqh_stream_read": [vp, sz, vp, vp],
+        "grinqh_kv_bytes": [ctypes.POINTER(KvDesc), ctypes.POINTER(sz), ctypes.POINTER(sz)],
+        "grinqh_kv_write": [ctypes.POINTER(KvDesc), ctypes.POINTER(_KvCache), ctypes.POINTER(_KvBatch),
+                            ctypes.c_int, ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), vp],
+        "grinqh_kv_read": [ctypes.POINTER(KvDesc), ctypes.POINTER(_KvCache), ctypes.POINTER(_KvBatch),
+                           ctypes.c_int, ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), vp],
+        "grinqh_attend_workspace_bytes": [ctypes.POINTER(KvDesc), ctypes.POINTER(AttendDesc), i32, i32,
+                                          ctypes.POINTER(sz)],
+        "grinqh_attend": [ctypes.POINTER(KvDesc), ctypes.POINTER(_KvCache), ctypes.POINTER(_KvBatch),
+                          ctypes.POINTER(AttendDesc), ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), vp, vp, sz, vp],
         "grinqh_vmm_topk": [dp, vp, vp, vp, i32, ctypes.POINTER(i32), vp, vp, i32, vp, sz, vp],
     }
     for name, args in sig.items():
@@ -449,3 +497,164 @@ def grinqh_stream_read(src, sink, stream=None):
     sp = _dev(src, torch.uint8, "src")
     kp = _dev(sink, torch.int32, "sink", (1,))
     _check(lib.grinqh_stream_read(sp, src.numel(), kp, _stream(stream)))
+
+
+# ------------------------------------------ key/value cache and attention --
+def make_kv_desc(format: int, heads: int, head_dim: int, page: int, n_pages: int) -> KvDesc:
+    return KvDesc(int(format), int(heads), int(head_dim), int(page), int(n_pages))
+
+
+def grinqh_kv_bytes(desc: KvDesc):
+    """(value bytes, scale bytes) of the arrays of K; those of V are the same."""
+    v, s = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib.grinqh_kv_bytes(ctypes.byref(desc), ctypes.byref(v), ctypes.byref(s)))
+    return int(v.value), int(s.value)
+
+
+def _kv_type(format):
+    torch = _torch()
+    return {GRINQH_KV_F16: torch.float16, GRINQH_KV_BF16: torch.bfloat16, GRINQH_KV_I8: torch.int8}[format]
+
+
+def _row_type(dtype, name):
+    torch = _torch()
+    types = {torch.float16: GRINQH_F16, torch.bfloat16: GRINQH_BF16, torch.float32: GRINQH_F32}
+    if dtype not in types:
+        raise TypeError(f"{name} must be fp16, bf16 or fp32, got {dtype}")
+    return types[dtype]
+
+
+def kv_cache(desc: KvDesc, device="cuda") -> KvCache:
+    """The arrays of a cache: zeros, so no page holds anything yet."""
+    torch = _torch()
+    grinqh_kv_bytes(desc)   # validates
+    shape = (desc.n_pages, desc.heads, desc.page)
+    dtype = _kv_type(desc.format)
+    values = [torch.zeros(shape + (desc.head_dim,), dtype=dtype, device=device) for _ in "kv"]
+    scales = [torch.zeros(shape, dtype=torch.float32, device=device) if desc.format == GRINQH_KV_I8 else None for _ in "kv"]
+    return KvCache(*values, *scales)
+
+
+def _cache_args(desc, cache):
+    torch = _torch()
+    grinqh_kv_bytes(desc)   # validates, so the shapes below mean something
+    shape = (desc.n_pages, desc.heads, desc.page)
+    dtype = _kv_type(desc.format)
+    c = _KvCache(_dev(cache.k, dtype, "cache.k", shape + (desc.head_dim,)),
+                 _dev(cache.v, dtype, "cache.v", shape + (desc.head_dim,)))
+    for n in ("k_scale", "v_scale"):
+        t = getattr(cache, n)
+        if t is not None:
+            setattr(c, n, _dev(t, torch.float32, "cache." + n, shape))
+    return c
+
+
+def _batch_args(batch, rows):
+    torch = _torch()
+    if batch.seq_lens.dim() != 1 or batch.block_table.dim() != 2:
+        raise ValueError("seq_lens must have one axis and block_table two")
+    B, width = int(batch.seq_lens.shape[0]), int(batch.block_table.shape[1])
+    return _KvBatch(_dev(batch.block_table, torch.int32, "block_table", (B, width)),
+                    _dev(batch.seq_lens, torch.int32, "seq_lens"),
+                    _dev(batch.row_offsets, torch.int32, "row_offsets", (B + 1,)), B, width, int(rows))
+
+
+def _rows(t, dtype, name, shape):
+    """A dense [rows, heads, head_dim] tensor: any strides, the last axis contiguous."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    r, h, d = t.stride()
+    if d != 1:
+        raise ValueError(f"{name} must be contiguous along head_dim")
+    return _Rows(t.data_ptr(), r, h)
+
+
+def _held_for(stream, *tensors):
+    """Tensors made here and used on a stream that is not the current one stay until it is done with them."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(stream)
+
+
+def grinqh_kv_write(desc: KvDesc, cache: KvCache, batch: KvBatch, k, v, stream=None) -> None:
+    """Write the batch's rows k and v [rows, heads, head_dim] (fp16, bf16 or fp32) into the cache."""
+    c = _cache_args(desc, cache)
+    shape = (int(k.shape[0]), desc.heads, desc.head_dim)
+    kr, vr = _rows(k, k.dtype, "k", shape), _rows(v, k.dtype, "v", shape)
+    b = _batch_args(batch, shape[0])
+    _check(lib.grinqh_kv_write(ctypes.byref(desc), ctypes.byref(c), ctypes.byref(b), _row_type(k.dtype, "k"),
+                               ctypes.byref(kr), ctypes.byref(vr), _stream(stream)))
+
+
+def grinqh_kv_read(desc: KvDesc, cache: KvCache, batch: KvBatch, rows: int, dtype=None, k=None, v=None, stream=None):
+    """(k, v) [rows, heads, head_dim] of `dtype` (fp16 by default), read back from the cache."""
+    torch = _torch()
+    c = _cache_args(desc, cache)
+    dtype = torch.float16 if dtype is None else dtype
+    shape = (int(rows), desc.heads, desc.head_dim)
+    b = _batch_args(batch, rows)
+    if k is None:
+        k = torch.empty(shape, dtype=dtype, device=cache.k.device)
+        _held_for(stream, k)
+    if v is None:
+        v = torch.empty(shape, dtype=dtype, device=cache.k.device)
+        _held_for(stream, v)
+    kr, vr = _rows(k, dtype, "k", shape), _rows(v, dtype, "v", shape)
+    _check(lib.grinqh_kv_read(ctypes.byref(desc), ctypes.byref(c), ctypes.byref(b), _row_type(dtype, "dtype"),
+                              ctypes.byref(kr), ctypes.byref(vr), _stream(stream)))
+    return k, v
+
+
+def _attend_desc(desc, heads, type, scale, window, sinks, max_rows, max_len):
+    if scale is None:
+        scale = float(desc.head_dim) ** -0.5
+    return AttendDesc(int(heads), type, float(scale), int(window), int(sinks), int(max_rows), int(max_len))
+
+
+def grinqh_attend_workspace_bytes(desc: KvDesc, heads: int, B: int, rows: int, max_rows: int, max_len: int,
+                                  window: int = 0, sinks: int = 0) -> int:
+    """Workspace that grinqh_attend needs for B sequences of `rows` rows in all."""
+    a = _attend_desc(desc, heads, GRINQH_BF16 if desc.format == GRINQH_KV_BF16 else GRINQH_F16, None, window, sinks,
+                     max_rows, max_len)
+    n = ctypes.c_size_t()
+    _check(lib.grinqh_attend_workspace_bytes(ctypes.byref(desc), ctypes.byref(a), int(B), int(rows), ctypes.byref(n)))
+    return int(n.value)
+
+
+def grinqh_attend(desc: KvDesc, cache: KvCache, batch: KvBatch, q, scale=None, window: int = 0, sinks: int = 0,
+                  max_rows=None, max_len=None, out=None, lse=None, workspace=None, stream=None):
+    """out [rows, heads, head_dim] of q's type: attention of the rows q over the cache (see grinqh.h).
+
+    max_rows and max_len bound the rows and the length of one sequence from above; they shape the launch only, and
+    default to the bounds that the shapes give.  lse (fp32 [rows, heads]) is written if it is passed."""
+    torch = _torch()
+    c = _cache_args(desc, cache)
+    if q.dim() != 3:
+        raise ValueError(f"q has shape {tuple(q.shape)}, expected [rows, heads, head_dim]")
+    rows, heads = int(q.shape[0]), int(q.shape[1])
+    shape = (rows, heads, desc.head_dim)
+    b = _batch_args(batch, rows)
+    if out is None:
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        _held_for(stream, out)
+    qr, outr = _rows(q, q.dtype, "q", shape), _rows(out, q.dtype, "out", shape)
+    lp = _dev(lse, torch.float32, "lse", (rows, heads)) if lse is not None else None
+    a = _attend_desc(desc, heads, _row_type(q.dtype, "q"), scale, window, sinks,
+                     max(1, rows) if max_rows is None else max_rows,
+                     max(1, min(b.table_width * desc.page, 1 << 30)) if max_len is None else max_len)
+    n = ctypes.c_size_t()
+    _check(lib.grinqh_attend_workspace_bytes(ctypes.byref(desc), ctypes.byref(a), b.B, rows, ctypes.byref(n)))
+    if workspace is None:
+        workspace = torch.empty(n.value, dtype=torch.uint8, device=q.device)
+        _held_for(stream, workspace)
+    wp = _dev(workspace, torch.uint8, "workspace") if workspace.numel() else None
+    _check(lib.grinqh_attend(ctypes.byref(desc), ctypes.byref(c), ctypes.byref(b), ctypes.byref(a), ctypes.byref(qr),
+                             ctypes.byref(outr), lp, wp, workspace.numel(), _stream(stream)))
+    return out
