@@ -1,0 +1,166 @@
+// What the attention kernels share (attend.hip, attend_rows.hip, attend_tile.hip).
+#pragma once
+
+#include "kv.h"
+
+namespace grinqh {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bhalf2 __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+
+
+// Results of the splits of a sequence: o [split][row * heads + head][D], normalised, and lse (base 2)
+// [split][row * heads + head]; o is not written where lse is -inf.
+struct Partial {
+  float* o;
+  float* lse;
+  long rows;        // rows * heads
+};
+
+// How a call is launched (attend.hip).
+struct AttendPlan {
+  bool tile;        // k_attend_tile, else k_attend_rows
+  int nb;           // k_attend_rows: blocks of 16 rows per wave
+  int blocks;       // row blocks of the longest sequence, as far as the caller's estimate goes
+  int splits;       // parts of a sequence's tiles, and tiles per part (the last takes the rest)
+  int per_split;
+};
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// The running maximum follows the scores once they pass it by this many powers of two, so weights
+// stay under 2^6 and the sums are rescaled a few times instead of at every tile.
+constexpr float kSlack = 6.0f;
+
+// The tiles of TK tokens that some of the rows at positions first .. last see: those of the sinks, then
+// from the window's start on.
+struct Span {
+  int sink_tiles, lo_tile, tiles, hi;   // hi: tokens from here on are seen by no row
+  __device__ __forceinline__ int tile(int v) const { return v < sink_tiles ? v : v - sink_tiles + lo_tile; }
+};
+
+template <int TK>
+__device__ __forceinline__ Span attend_span(const Attend& a, int first, int last) {
+  Span s;
+  s.hi = max(last + 1, 0);
+  const int lo = a.window ? min(max(first - a.window + 1, 0), s.hi) : 0;
+  s.lo_tile = lo / TK;
+  s.sink_tiles = min((min(a.sinks, s.hi) + TK - 1) / TK, s.lo_tile);
+  s.tiles = s.sink_tiles + (s.hi + TK - 1) / TK - s.lo_tile;
+  return s;
+}
+
+// Whether every row at positions first .. last sees every token of t0 .. t0 + n - 1.
+__device__ __forceinline__ bool all_visible(const Attend& a, int first, int last, int t0, int n) {
+  return t0 + n - 1 <= first && (!a.window || t0 > last - a.window || t0 + n <= a.sinks);
+}
+
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {   // to nearest even
+  if constexpr (TYPE == GRINQH_F16) {
+    half2 r;
+    r[0] = (_Float16)x; r[1] = (_Float16)y;
+    return __builtin_bit_cast(uint32_t, r);
+  } else {
+    bhalf2 r;
+    r[0] = (__bf16)x; r[1] = (__bf16)y;
+    return __builtin_bit_cast(uint32_t, r);
+  }
+}
+
+// 16-bit formats: whether a dword holds a value that is not finite, as a mask of its halves.
+template <int FORMAT>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  constexpr uint32_t e = FORMAT == GRINQH_KV_F16 ? 0x7c00u : 0x7f80u;
+  return ((w & e) == e ? 0xffffu : 0u) | ((w >> 16 & e) == e ? 0xffff0000u : 0u);
+}
+
+// What a value that is not finite adds where it is seen: 1 in the halves of w that are +inf or NaN
+// (sign = 0), -inf or NaN (sign = 1).
+template <int FORMAT>
+__device__ __forceinline__ uint32_t infinite_ones(uint32_t w, int sign) {
+  constexpr uint32_t one = FORMAT == GRINQH_KV_F16 ? 0x3c00u : 0x3f80u;
+  constexpr uint32_t inf = FORMAT == GRINQH_KV_F16 ? 0x7c00u : 0x7f80u;
+  uint32_t r = 0;
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t h = w >> (16 * i) & 0xffffu;
+    const bool nan = (h & 0x7fffu) > inf;
+    if (nan || h == (inf | (uint32_t)sign << 15)) r |= one << (16 * i);
+  }
+  return r;
+}
+
+template <int FORMAT>
+__device__ __forceinline__ float4v mfma16(u32x4 a, u32x4 b, float4v c) {
+  if constexpr (FORMAT == GRINQH_KV_BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8, a), __builtin_bit_cast(bhalf8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+
+template <int FORMAT>
+__device__ __forceinline__ float16v mfma32(u32x4 a, u32x4 b, float16v c) {
+  if constexpr (FORMAT == GRINQH_KV_BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bhalf8, a), __builtin_bit_cast(bhalf8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+
+// Maximum over the lanes that differ in bit 5, and in bit 4, of the lane number.
+__device__ __forceinline__ float max_xor32(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float max_xor16(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float sum_xor32(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float sum_xor16(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// Two int8 codes as fp16, exact: bytes a and b of w ^ 0x80808080 beside 0x64 read as 1024 + code + 128.
+__device__ __forceinline__ uint32_t codes2(uint32_t offset_binary, uint32_t a, uint32_t b) {
+  const uint32_t v = __builtin_amdgcn_perm(0x64646464u, offset_binary, a | 0x0400u | (b << 16) | 0x04000000u);
+  const half2 c = {(_Float16)1152.0f, (_Float16)1152.0f};
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2, v) - c);
+}
+
+// Queries of a row for the products with an 8-bit cache: fp16 as they are, bf16 as fp16 times the power of
+// two that brings the row's largest magnitude to 2^14..2^15 (exact but for what lies 2^28 below it).
+__device__ __forceinline__ int row_shift(float amax) {
+  return amax > 0 && amax < INFINITY ? 14 - ilogbf(amax) : 0;
+}
+
+// The exponent a positive finite scale is held against: scale <= 2^e.
+__device__ __forceinline__ int scale_exponent(float s) {
+  return (int)(__builtin_bit_cast(uint32_t, s) >> 23 & 0xffu) - 126;
+}
+// Values of an 8-bit cache are weighed by exp(s - m) * scale * 2^(kUp - e), e the exponent of the largest
+// finite scale that the row has seen so far: at most 2^15 in fp16, and 11 bits stay down to scales 2^23
+// below it.  The sum that divides carries the same factor.  Stored scales reach down to 2^-107; the floor
+// keeps that sum inside fp32.
+constexpr int kUp = 9;
+constexpr int kLowestExponent = -90;
+
+size_t partial_bytes(const AttendPlan& p, const KvCache& c, const Attend& a, int rows);
+void launch_attend_rows(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q,
+                        const DenseRows& out, float* lse, const Partial& part, hipStream_t s);
+void launch_attend_tile(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q,
+                        const DenseRows& out, float* lse, const Partial& part, hipStream_t s);
+
+}  // namespace grinqh

@@ -1,84 +1,85 @@
-// Attention of a batch's rows over the paged cache.
-#include "kv.h"
+// Attention of a batch's rows over the paged cache: how a call is launched,
+// and the joining of sequences that were split.
+#include "attend.h"
+
+#include <algorithm>
 
 namespace grinqh {
 
-// One wave per row and query head: lane = token for the scores, lane = channel
-// for the sum over the values.  Running maximum and sum in fp32.
-template <int D, int FORMAT, int TYPE>
-__global__ void k_attend_simple(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, float* lse) {
-  const int lane = threadIdx.x, head = blockIdx.x, s = blockIdx.z, h = head / a.G;
+namespace {
+
+// One group of D / 8 lanes per row and head: the splits' results weighed by their sums.
+template <int D, int TYPE>
+__global__ void k_attend_join(KvCache c, KvBatch b, Attend a, DenseRows out, float* lse, Partial part, int splits) {
+  constexpr int LPR = D / 8;
+  const int s = blockIdx.z, lane = threadIdx.x % LPR;
   const Seq sq = kv_seq(c, b, s);
-  for (int i = blockIdx.y; i < sq.n; i += gridDim.y) {
-    const int row = sq.r0 + i, p = sq.L - sq.n + i;
-    const uint16_t* qp = (const uint16_t*)q.p + row * q.row + head * q.head;
-    const int lo = a.window ? max(0, p - a.window + 1) : 0, first = min(a.sinks, lo);
-    float m = -INFINITY, l = 0, o[D / 64] = {};
-    for (int t0 = 0; t0 <= p; t0 += 64) {
-      if (t0 >= first && t0 + 63 < lo) continue;
-      const int t = t0 + lane;
-      const bool sees = t <= p && (t >= lo || t < first);
-      const int page = sees ? kv_page(c, b, s, t) : -1;
-      const long slot = page >= 0 ? kv_slot(c, page, h, t) : 0;
-      float x = sees ? NAN : -INFINITY;
-      if (page >= 0) {
-        x = 0;
-        for (int d = 0; d < D; ++d) {
-          const float qd = TYPE == GRINQH_F16 ? h2f(qp[d]) : bf2f(qp[d]);
-          if (FORMAT == GRINQH_KV_I8) x += qd * (float)((const int8_t*)c.k)[slot * D + d];
-          else {
-            const uint16_t kd = ((const uint16_t*)c.k)[slot * D + d];
-            x += qd * (FORMAT == GRINQH_KV_F16 ? h2f(kd) : bf2f(kd));
-          }
-        }
-        x *= a.scale;
-        if (FORMAT == GRINQH_KV_I8) x *= c.ks[slot];
-      }
-      float mx = x;
-      for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-      const float mn = fmaxf(m, mx), base = mn == -INFINITY ? 0.0f : mn;
-      const float alpha = expf(m - base);
-      const float e = sees ? expf(x - base) : 0.0f;
-      float sum = e;
-      for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-      l = l * alpha + sum;
-      m = mn;
-      for (int j = 0; j < D / 64; ++j) o[j] *= alpha;
-      for (int u = 0; u < 64; ++u) {
-        const float pu = __shfl(e, u);
-        const long su = __shfl(slot, u);
-        if (!__shfl((int)sees, u)) continue;
-        const float w = FORMAT == GRINQH_KV_I8 ? pu * c.vs[su] : pu;
-        for (int j = 0; j < D / 64; ++j) {
-          const long at = su * D + j * 64 + lane;
-          float vd;
-          if (FORMAT == GRINQH_KV_I8) vd = (float)((const int8_t*)c.v)[at];
-          else vd = FORMAT == GRINQH_KV_F16 ? h2f(((const uint16_t*)c.v)[at]) : bf2f(((const uint16_t*)c.v)[at]);
-          o[j] += w * vd;
-        }
-      }
+  const long all = (long)sq.n * a.heads;
+  const int per_block = blockDim.x / LPR;
+  for (long r = (long)blockIdx.x * per_block + threadIdx.x / LPR; r < all; r += (long)gridDim.x * per_block) {
+    const long at = (long)sq.r0 * a.heads + r;
+    float m = -INFINITY;
+    for (int i = lane; i < splits; i += LPR) m = fmaxf(m, part.lse[i * part.rows + at]);
+    for (int x = LPR / 2; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, LPR));
+    const float base = m == -INFINITY ? 0.0f : m;
+    float sum = 0, y[8] = {};
+    for (int i = 0; i < splits; ++i) {
+      const float z = part.lse[i * part.rows + at];
+      if (z == -INFINITY) continue;
+      const float w = exp2f(z - base);
+      const float4v* p = (const float4v*)(part.o + (i * part.rows + at) * D + lane * 8);
+      sum += w;
+      for (int j = 0; j < 8; ++j) y[j] += w * p[j / 4][j % 4];
     }
-    const float inv = l == 0 ? 0.0f : 1.0f / l;
-    uint16_t* op = (uint16_t*)out.p + row * out.row + head * out.head;
-    for (int j = 0; j < D / 64; ++j) {
-      const float y = o[j] * inv;
-      op[j * 64 + lane] = TYPE == GRINQH_F16 ? f2h_rn(y) : f2bf_rn(y);
-    }
-    if (lse && lane == 0) lse[(long)row * a.heads + head] = l == 0 ? -INFINITY : m + logf(l);
+    const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+    uint32_t w[4];
+    for (int j = 0; j < 4; ++j) w[j] = pack2<TYPE>(y[2 * j] * inv, y[2 * j + 1] * inv);
+    *(u32x4*)(out.p + ((sq.r0 + r / a.heads) * out.row + (r % a.heads) * out.head + lane * 8) * 2) = u32x4{w[0], w[1], w[2], w[3]};
+    if (lse && lane == 0) lse[at] = sum == 0 ? -INFINITY : (m + log2f(sum)) * kLn2;
   }
 }
 
-size_t attend_workspace(const KvCache&, const Attend&, int, int) { return 0; }
+AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
+  AttendPlan p = {};
+  const long n = std::min(a.max_rows, rows), R = n * a.G;
+  p.nb = R > 16 ? 2 : 1;
+  p.blocks = (int)std::min<long>((R + 16 * p.nb - 1) / (16 * p.nb), 65535);
+  // tiles that the longest sequence's last block sees
+  const long seen = a.window ? std::min<long>(a.max_len, (long)a.window + n + a.sinks + 64) : a.max_len;
+  const long tiles = (seen + 31) / 32, groups = (long)B * c.H * p.blocks;
+  long splits = std::max<long>(1, 2L * device_cus() / groups);
+  splits = std::min(splits, std::max<long>(1, tiles / 8));
+  long per = (tiles + splits - 1) / splits;
+  per = (per + 3) / 4 * 4;
+  p.per_split = (int)per;
+  p.splits = (int)((tiles + per - 1) / per);
+  return p;
+}
+
+}  // namespace
+
+size_t partial_bytes(const AttendPlan& p, const KvCache& c, const Attend& a, int rows) {
+  return p.splits > 1 ? (size_t)p.splits * rows * a.heads * (c.D + 1) * sizeof(float) : 0;
+}
+
+size_t attend_workspace(const KvCache& c, const Attend& a, int B, int rows) {
+  return partial_bytes(attend_plan(c, a, B, rows), c, a, rows);
+}
 
 int launch_attend(const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q, const DenseRows& out,
-                  float* lse, void*, hipStream_t s) {
-  const dim3 grid(a.heads, min(min(a.max_rows, b.rows), 32768), b.B);
+                  float* lse, void* workspace, hipStream_t s) {
+  const AttendPlan p = attend_plan(c, a, b.B, b.rows);
+  Partial part = {(float*)workspace, nullptr, (long)b.rows * a.heads};
+  part.lse = part.o + p.splits * part.rows * c.D;
+  launch_attend_rows(p, c, b, a, q, out, lse, part, s);
+  int st = check_launch("attend");
+  if (st || p.splits == 1) return st;
+  const long per_seq = (long)std::min(a.max_rows, b.rows) * a.heads * (c.D / 8);
+  const dim3 grid((unsigned)std::min<long>((per_seq + 255) / 256, 1 << 20), 1, b.B);
   auto go = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (c.format == GRINQH_KV_F16) k_attend_simple<D, GRINQH_KV_F16, GRINQH_F16><<<grid, 64, 0, s>>>(c, b, a, q, out, lse);
-    else if (c.format == GRINQH_KV_BF16) k_attend_simple<D, GRINQH_KV_BF16, GRINQH_BF16><<<grid, 64, 0, s>>>(c, b, a, q, out, lse);
-    else if (a.type == GRINQH_F16) k_attend_simple<D, GRINQH_KV_I8, GRINQH_F16><<<grid, 64, 0, s>>>(c, b, a, q, out, lse);
-    else k_attend_simple<D, GRINQH_KV_I8, GRINQH_BF16><<<grid, 64, 0, s>>>(c, b, a, q, out, lse);
+    if (a.type == GRINQH_F16) k_attend_join<D, GRINQH_F16><<<grid, 256, 0, s>>>(c, b, a, out, lse, part, p.splits);
+    else k_attend_join<D, GRINQH_BF16><<<grid, 256, 0, s>>>(c, b, a, out, lse, part, p.splits);
   };
   if (c.D == 64) go(std::integral_constant<int, 64>{});
   else go(std::integral_constant<int, 128>{});

@@ -5,6 +5,9 @@
 
 namespace grinqh {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr long kMaxTokens = 1L << 30;   // of a sequence: token indices and a tile beyond them fit 32 bits
 
 // A validated cache, passed to kernels by value.

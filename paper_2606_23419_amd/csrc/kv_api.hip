@@ -82,7 +82,10 @@ static int resolve_attend(const KvCache& c, const grinqh_attend_desc* d, Attend*
   if (d->window < 0 || d->sinks < 0) return fail(GRINQH_EINVAL, "window=%d and sinks=%d must not be negative", d->window, d->sinks);
   if (d->max_rows < 1 || d->max_len < 1)
     return fail(GRINQH_EINVAL, "max_rows=%d and max_len=%d must be positive", d->max_rows, d->max_len);
-  *a = Attend{d->heads, d->heads / c.H, d->type, d->scale, d->window, d->window ? d->sinks : 0, d->max_rows, d->max_len};
+  // no length passes kMaxTokens: a window of that many tokens hides nothing
+  const int window = d->window < kMaxTokens ? d->window : 0;
+  const int sinks = window ? (int)(d->sinks < kMaxTokens ? d->sinks : kMaxTokens) : 0;
+  *a = Attend{d->heads, d->heads / c.H, d->type, d->scale, window, sinks, d->max_rows, d->max_len};
   return GRINQH_OK;
 }
 

@@ -3,8 +3,6 @@
 
 namespace grinqh {
 
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Eight consecutive values of a dense row.
 template <int TYPE>
