@@ -12,7 +12,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgrinqh.so")
 SOURCES = ["grinqh_api.hip", "pack.hip", "assign.hip", "vmm.hip", "vmm_dot2.hip", "vmm_pp.hip",
            "vmm_mm.hip", "prefill.hip", "prefill_small.hip", "vmm_lut.hip", "kv_api.hip", "kv_cache.hip",
-           "attend.hip", "attend_rows.hip"]
+           "attend.hip", "attend_rows.hip", "attend_tile.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

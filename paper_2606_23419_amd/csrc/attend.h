@@ -25,7 +25,7 @@ struct Partial {
 // How a call is launched (attend.hip).
 struct AttendPlan {
   bool tile;        // k_attend_tile, else k_attend_rows
-  int nb;           // k_attend_rows: blocks of 16 rows per wave
+  int nb;           // k_attend_rows: blocks of 16 rows per wave; k_attend_tile: waves of 32 rows
   int blocks;       // row blocks of the longest sequence, as far as the caller's estimate goes
   int splits;       // parts of a sequence's tiles, and tiles per part (the last takes the rest)
   int per_split;
@@ -80,20 +80,6 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   return ((w & e) == e ? 0xffffu : 0u) | ((w >> 16 & e) == e ? 0xffff0000u : 0u);
 }
 
-// What a value that is not finite adds where it is seen: 1 in the halves of w that are +inf or NaN
-// (sign = 0), -inf or NaN (sign = 1).
-template <int FORMAT>
-__device__ __forceinline__ uint32_t infinite_ones(uint32_t w, int sign) {
-  constexpr uint32_t one = FORMAT == GRINQH_KV_F16 ? 0x3c00u : 0x3f80u;
-  constexpr uint32_t inf = FORMAT == GRINQH_KV_F16 ? 0x7c00u : 0x7f80u;
-  uint32_t r = 0;
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t h = w >> (16 * i) & 0xffffu;
-    const bool nan = (h & 0x7fffu) > inf;
-    if (nan || h == (inf | (uint32_t)sign << 15)) r |= one << (16 * i);
-  }
-  return r;
-}
 
 template <int FORMAT>
 __device__ __forceinline__ float4v mfma16(u32x4 a, u32x4 b, float4v c) {
@@ -152,10 +138,9 @@ __device__ __forceinline__ int scale_exponent(float s) {
 }
 // Values of an 8-bit cache are weighed by exp(s - m) * scale * 2^(kUp - e), e the exponent of the largest
 // finite scale that the row has seen so far: at most 2^15 in fp16, and 11 bits stay down to scales 2^23
-// below it.  The sum that divides carries the same factor.  Stored scales reach down to 2^-107; the floor
-// keeps that sum inside fp32.
+// below it.  Stored scales reach down to 2^-107.
 constexpr int kUp = 9;
-constexpr int kLowestExponent = -90;
+constexpr int kLowestExponent = -110;
 
 size_t partial_bytes(const AttendPlan& p, const KvCache& c, const Attend& a, int rows);
 void launch_attend_rows(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q,

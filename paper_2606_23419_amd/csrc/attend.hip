@@ -41,16 +41,19 @@ __global__ void k_attend_join(KvCache c, KvBatch b, Attend a, DenseRows out, flo
 
 AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
   AttendPlan p = {};
+  const int forced = option(&Options::attend_kernel), forced_splits = option(&Options::attend_splits);
   const long n = std::min(a.max_rows, rows), R = n * a.G;
-  p.nb = R > 16 ? 2 : 1;
-  p.blocks = (int)std::min<long>((R + 16 * p.nb - 1) / (16 * p.nb), 65535);
+  p.tile = forced ? forced != GRINQH_ATTEND_ROWS : R > 32;
+  p.nb = p.tile ? (forced == GRINQH_ATTEND_TILE_4 ? 4 : 8) : R > 16 ? 2 : 1;
+  const long per_block = p.tile ? 32 * p.nb : 16 * p.nb, tile = p.tile ? 64 : 32;
+  p.blocks = (int)std::min<long>((R + per_block - 1) / per_block, 65535);
   // tiles that the longest sequence's last block sees
-  const long seen = a.window ? std::min<long>(a.max_len, (long)a.window + n + a.sinks + 64) : a.max_len;
-  const long tiles = (seen + 31) / 32, groups = (long)B * c.H * p.blocks;
-  long splits = std::max<long>(1, 2L * device_cus() / groups);
-  splits = std::min(splits, std::max<long>(1, tiles / 8));
+  const long seen = a.window ? std::min<long>(a.max_len, (long)a.window + per_block / a.G + a.sinks + 2 * tile) : a.max_len;
+  const long tiles = (seen + tile - 1) / tile, groups = (long)B * c.H * p.blocks;
+  const long fill = p.tile ? (p.nb == 4 ? 2 : 1) * device_cus() : 2 * device_cus();
+  long splits = forced_splits ? forced_splits : std::min(std::max<long>(1, fill / groups), std::max<long>(1, tiles / 8));
   long per = (tiles + splits - 1) / splits;
-  per = (per + 3) / 4 * 4;
+  if (!p.tile) per = (per + 3) / 4 * 4;
   p.per_split = (int)per;
   p.splits = (int)((tiles + per - 1) / per);
   return p;
@@ -71,7 +74,7 @@ int launch_attend(const KvCache& c, const KvBatch& b, const Attend& a, const Den
   const AttendPlan p = attend_plan(c, a, b.B, b.rows);
   Partial part = {(float*)workspace, nullptr, (long)b.rows * a.heads};
   part.lse = part.o + p.splits * part.rows * c.D;
-  launch_attend_rows(p, c, b, a, q, out, lse, part, s);
+  (p.tile ? launch_attend_tile : launch_attend_rows)(p, c, b, a, q, out, lse, part, s);
   int st = check_launch("attend");
   if (st || p.splits == 1) return st;
   const long per_seq = (long)std::min(a.max_rows, b.rows) * a.heads * (c.D / 8);

@@ -31,6 +31,21 @@ __device__ const uint32_t g_filler[2][64] = {
      0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
      0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff}};
 
+// What a value that is not finite adds where it is seen: 1 in the halves of w that are +inf or NaN
+// (sign = 0), -inf or NaN (sign = 1).
+template <int FORMAT>
+__device__ __forceinline__ uint32_t infinite_ones(uint32_t w, int sign) {
+  constexpr uint32_t one = FORMAT == GRINQH_KV_F16 ? 0x3c00u : 0x3f80u;
+  constexpr uint32_t inf = FORMAT == GRINQH_KV_F16 ? 0x7c00u : 0x7f80u;
+  uint32_t r = 0;
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t h = w >> (16 * i) & 0xffffu;
+    const bool nan = (h & 0x7fffu) > inf;
+    if (nan || h == (inf | (uint32_t)sign << 15)) r |= one << (16 * i);
+  }
+  return r;
+}
+
 __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
@@ -253,12 +268,12 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
         if (__any(rises || grows)) {
           float alpha = rises ? exp2f(m[n] - mx) : 1.0f;
           if (rises) m[n] = mx;
-          if (grows) { alpha *= ldexpf(1.0f, max(ev[n] - big, -126)); ev[n] = big; }
           l[n] *= alpha;
+          if (grows) { alpha *= ldexpf(1.0f, max(ev[n] - big, -126)); ev[n] = big; }
 #pragma unroll
           for (int j = 0; j < VC; ++j) o[n][j] *= alpha;
         }
-        const float base = (m[n] == -INFINITY ? 0.0f : m[n]) + (I8 ? (float)(ev[n] - kUp) : 0.0f);
+        const float base = m[n] == -INFINITY ? 0.0f : m[n], down = I8 ? ldexpf(1.0f, kUp - ev[n]) : 1.0f;
         float p[8];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -267,7 +282,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
             float x = __builtin_amdgcn_exp2f(fmaf(sc[n][t][e], factor[n], -base));
             l[n] += x;
             if constexpr (I8) {
-              x *= vst[t][e];
+              x *= vst[t][e] * down;
               if (!whole && !vis[t][e]) x = 0;   // a scale that is not finite stays with the rows that see it
             }
             p[4 * t + e] = x;
@@ -345,7 +360,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
     float up[NB];   // what brings the sums over the values back
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      l[n] = sum_xor16(sum_xor32(l[n])) * (I8 ? ldexpf(1.0f, ev[n] - kUp) : 1.0f);
+      l[n] = sum_xor16(sum_xor32(l[n]));
       up[n] = I8 ? ldexpf(1.0f, ev[n]) : 1.0f;
       if (quad == 0) { lds.m[wave][16 * n + i16] = m[n]; lds.l[wave][16 * n + i16] = l[n]; }
     }

@@ -80,6 +80,8 @@ struct Options {
   int prefill_tile;     // 1..3: 256x256, 256x128, 128x128
   int lut_groups;       // groups per workgroup of the LUT VMM
   int prefill_cus;      // CUs the prefill counts its rounds in (0: the device's)
+  int attend_kernel;    // GRINQH_ATTEND_*: the attention kernel
+  int attend_splits;    // parts that a sequence's tokens are split into
 };
 int option(int Options::*field);
 

@@ -272,6 +272,52 @@ def test_attend(g, torch, fmt, type, D, H, G, page, seqs):
     c.check(*c.attend())
 
 
+@pytest.fixture(params=["rows", "tile4", "tile8", "tile8x3", "rowsx3"])
+def forced(g, request):
+    """Every kernel on its own, and sequences split in three whatever their size."""
+    kernel = {"rows": g.GRINQH_ATTEND_ROWS, "tile4": g.GRINQH_ATTEND_TILE_4, "tile8": g.GRINQH_ATTEND_TILE_8}
+    name, _, splits = request.param.partition("x")
+    g.grinqh_set_option(g.GRINQH_OPT_ATTEND_KERNEL, kernel[name])
+    g.grinqh_set_option(g.GRINQH_OPT_ATTEND_SPLITS, int(splits or 0))
+    yield request.param
+    g.grinqh_set_option(g.GRINQH_OPT_ATTEND_KERNEL, 0)
+    g.grinqh_set_option(g.GRINQH_OPT_ATTEND_SPLITS, 0)
+
+
+@pytest.mark.parametrize("fmt,type", FORMATS)
+@pytest.mark.parametrize("D,G,page", [(128, 4, 16), (64, 3, 2)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (50, 5)])
+def test_every_kernel(g, torch, forced, fmt, type, D, G, page, window, sinks):
+    seqs = [(1, 1), (90, 300), (0, 3), (1, 500), (9, 4), (64, 64)]
+    c = Case(g, torch, seqs, fmt=fmt, type=type, D=D, H=2, G=G, page=page, fill=float("nan")).upload()
+    out, lse = c.attend(window=window, sinks=sinks, max_rows=90, max_len=500)
+    c.check(out, lse, window, sinks)
+
+
+@pytest.mark.parametrize("fmt,type", [("f16", "f16"), ("bf16", "bf16"), ("i8", "f16")])
+def test_masked_infinities_in_every_kernel(g, torch, forced, fmt, type):
+    """Values of all three kinds at one channel each, seen by the later rows of a chunk only."""
+    n, L, window = 100, 130, 40
+    bad = {3: float("inf"), 40: -float("inf"), 77: float("nan")}
+    for t in (35, 64, 99, 127):
+        c = Case(g, torch, [(n, L)], fmt=fmt, type=type, H=1, G=2, page=16, seed=5)
+        if fmt == "i8":
+            c.scales["v"][c.table[0, t // 16], :, t % 16] = float("nan")
+        else:
+            for d, x in bad.items():
+                c.pool["v"][c.table[0, t // 16], :, t % 16, d] = x
+        c.upload()
+        got = down(c.attend(window=window)[0])
+        seen = kv.sees(np.arange(L - n, L), t, window, 0)
+        assert np.isfinite(got[~seen]).all()
+        if fmt == "i8":
+            assert np.isnan(got[seen]).all()
+        else:
+            for d, x in bad.items():
+                assert np.array_equal(got[seen][..., d], np.full_like(got[seen][..., d], x), equal_nan=True)
+            assert np.isfinite(np.delete(got, list(bad), axis=-1)).all()
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (5, 0), (16, 4), (63, 1), (64, 64), (100, 7), (65, 200), (1000, 4)])
 @pytest.mark.parametrize("fmt,type", [("i8", "f16"), ("bf16", "bf16")])
 def test_window_and_sinks(g, torch, fmt, type, window, sinks):
