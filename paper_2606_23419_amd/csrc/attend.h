@@ -31,6 +31,36 @@ struct AttendPlan {
   int per_split;
 };
 
+// A load known to be from device memory: through a pointer that may point to more than one array the
+// compiler would use a flat load, which every wait for LDS would wait for as well.
+template <typename T>
+__device__ __forceinline__ T load_global(const void* p) {
+  return *(const __attribute__((address_space(1))) T*)p;
+}
+
+// The attention kernels' argument.  What only the start or the end of a kernel needs is read there (late()):
+// held in scalar registers throughout, it would push other values out of them.
+struct AttendArgs {
+  KvCache c;
+  KvBatch b;
+  Attend a;
+  int splits, per_split;
+  DenseRows q, out;
+  float* lse;
+  Partial part;
+};
+
+__device__ __forceinline__ const AttendArgs& late() {
+  auto p = (const __attribute__((address_space(4))) AttendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));   // keeps the loads where they are asked for
+  return *(const AttendArgs*)p;
+}
+
+// Waves per workgroup of k_attend_rows, and per SIMD: of one block of 16 rows three (8-bit) or two workgroups of
+// four waves share a CU, so that one's start and end overlap with the others' loads.
+constexpr int rows_waves(int nb) { return nb == 1 ? 4 : 8; }
+constexpr int rows_per_simd(int format, int nb) { return format == GRINQH_KV_I8 && nb == 1 ? 3 : 2; }
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once they pass it by this many powers of two, so weights
@@ -53,6 +83,12 @@ __device__ __forceinline__ Span attend_span(const Attend& a, int first, int last
   s.sink_tiles = min((min(a.sinks, s.hi) + TK - 1) / TK, s.lo_tile);
   s.tiles = s.sink_tiles + (s.hi + TK - 1) / TK - s.lo_tile;
   return s;
+}
+
+// What a row at position pos sees: token t if t <= pos and t lies past behind_window or before the sinks' end.
+__device__ __forceinline__ int behind_window(const Attend& a, int pos) { return a.window ? pos - a.window : -0x7fffffff - 1; }
+__device__ __forceinline__ bool row_sees(int t, int pos, int behind, int sinks) {
+  return (t <= pos) & ((t > behind) | (t < sinks));   // without branches
 }
 
 // Whether every row at positions first .. last sees every token of t0 .. t0 + n - 1.
@@ -78,6 +114,12 @@ template <int FORMAT>
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   constexpr uint32_t e = FORMAT == GRINQH_KV_F16 ? 0x7c00u : 0x7f80u;
   return ((w & e) == e ? 0xffffu : 0u) | ((w >> 16 & e) == e ? 0xffff0000u : 0u);
+}
+
+// The larger of each half, as unsigned numbers.
+__device__ __forceinline__ uint32_t max_halves(uint32_t x, uint32_t y) {
+  typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, x), __builtin_bit_cast(ushort2v, y)));
 }
 
 
@@ -132,20 +174,18 @@ __device__ __forceinline__ int row_shift(float amax) {
   return amax > 0 && amax < INFINITY ? 14 - ilogbf(amax) : 0;
 }
 
-// The exponent a positive finite scale is held against: scale <= 2^e.
+// The exponent a scale >= 0 is held against: scale <= 2^e.  (An infinite one makes every channel of the rows that
+// see it infinite or NaN, whatever it is held against.)
 __device__ __forceinline__ int scale_exponent(float s) {
   return (int)(__builtin_bit_cast(uint32_t, s) >> 23 & 0xffu) - 126;
 }
 // Values of an 8-bit cache are weighed by exp(s - m) * scale * 2^(kUp - e), e the exponent of the largest
-// finite scale that the row has seen so far: at most 2^15 in fp16, and 11 bits stay down to scales 2^23
+// scale that the row has seen so far: at most 2^15 in fp16, and 11 bits stay down to scales 2^23
 // below it.  Stored scales reach down to 2^-107.
 constexpr int kUp = 9;
 constexpr int kLowestExponent = -110;
 
-size_t partial_bytes(const AttendPlan& p, const KvCache& c, const Attend& a, int rows);
-void launch_attend_rows(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q,
-                        const DenseRows& out, float* lse, const Partial& part, hipStream_t s);
-void launch_attend_tile(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q,
-                        const DenseRows& out, float* lse, const Partial& part, hipStream_t s);
+void launch_attend_rows(const AttendPlan& p, const AttendArgs& args, hipStream_t s);
+void launch_attend_tile(const AttendPlan& p, const AttendArgs& args, hipStream_t s);
 
 }  // namespace grinqh

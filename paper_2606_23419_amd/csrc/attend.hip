@@ -8,34 +8,78 @@ namespace grinqh {
 
 namespace {
 
-// One group of D / 8 lanes per row and head: the splits' results weighed by their sums.
+// The splits' results of a row and head, weighed by their sums.  D / 8 lanes hold the channels; `groups` such
+// groups of a workgroup take every groups-th split of one row and meet in LDS, so a row of many splits is not
+// one chain of loads.
+constexpr int kJoinThreads = 256;
+
 template <int D, int TYPE>
-__global__ void k_attend_join(KvCache c, KvBatch b, Attend a, DenseRows out, float* lse, Partial part, int splits) {
-  constexpr int LPR = D / 8;
-  const int s = blockIdx.z, lane = threadIdx.x % LPR;
+__global__ __launch_bounds__(kJoinThreads) void k_attend_join(KvCache c, KvBatch b, Attend a, DenseRows out, float* lse,
+                                                              Partial part, int splits, int groups) {
+  constexpr int LPR = D / 8, GROUPS = kJoinThreads / LPR;
+  __shared__ float sm[GROUPS], ssum[GROUPS], sy[GROUPS][D];
+  const int s = blockIdx.z, lane = threadIdx.x % LPR, group = threadIdx.x / LPR, g = group % groups;
   const Seq sq = kv_seq(c, b, s);
   const long all = (long)sq.n * a.heads;
-  const int per_block = blockDim.x / LPR;
-  for (long r = (long)blockIdx.x * per_block + threadIdx.x / LPR; r < all; r += (long)gridDim.x * per_block) {
-    const long at = (long)sq.r0 * a.heads + r;
-    float m = -INFINITY;
-    for (int i = lane; i < splits; i += LPR) m = fmaxf(m, part.lse[i * part.rows + at]);
-    for (int x = LPR / 2; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, LPR));
-    const float base = m == -INFINITY ? 0.0f : m;
-    float sum = 0, y[8] = {};
-    for (int i = 0; i < splits; ++i) {
-      const float z = part.lse[i * part.rows + at];
-      if (z == -INFINITY) continue;
-      const float w = exp2f(z - base);
-      const float4v* p = (const float4v*)(part.o + (i * part.rows + at) * D + lane * 8);
-      sum += w;
-      for (int j = 0; j < 8; ++j) y[j] += w * p[j / 4][j % 4];
+  const int per_block = GROUPS / groups;
+  for (long r0 = (long)blockIdx.x * per_block; r0 < all; r0 += (long)gridDim.x * per_block) {
+    const long r = r0 + group / groups, at = (long)sq.r0 * a.heads + min(r, all - 1);
+    float m = -INFINITY, sum = 0, y[8] = {};
+    // four splits in flight; past the last one the last is read again and weighs nothing
+    for (int i0 = g; i0 < splits; i0 += 4 * groups) {
+      float z[4];
+      float4v p[4][2];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const long i = min(i0 + u * groups, splits - 1);
+        z[u] = part.lse[i * part.rows + at];
+        const float4v* src = (const float4v*)(part.o + (i * part.rows + at) * D + lane * 8);
+        p[u][0] = src[0];
+        p[u][1] = src[1];
+      }
+      float top = m;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i0 + u * groups >= splits) z[u] = -INFINITY;
+        top = fmaxf(top, z[u]);
+      }
+      const float base = top == -INFINITY ? 0.0f : top, old = exp2f(m - base);
+      m = top;
+      sum *= old;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] *= old;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool any = z[u] != -INFINITY;   // else nothing was written there
+        const float w = any ? exp2f(z[u] - base) : 0.0f;
+        sum += w;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] += any ? w * p[u][j >> 2][j & 3] : 0.0f;
+      }
     }
-    const float inv = sum == 0 ? 0.0f : 1.0f / sum;
-    uint32_t w[4];
-    for (int j = 0; j < 4; ++j) w[j] = pack2<TYPE>(y[2 * j] * inv, y[2 * j + 1] * inv);
-    *(u32x4*)(out.p + ((sq.r0 + r / a.heads) * out.row + (r % a.heads) * out.head + lane * 8) * 2) = u32x4{w[0], w[1], w[2], w[3]};
-    if (lse && lane == 0) lse[at] = sum == 0 ? -INFINITY : (m + log2f(sum)) * kLn2;
+    if (groups > 1) {
+      if (lane == 0) { sm[group] = m; ssum[group] = sum; }
+      for (int j = 0; j < 8; ++j) sy[group][lane * 8 + j] = y[j];
+      __syncthreads();
+      float top = -INFINITY;
+      for (int i = 0; i < groups; ++i) top = fmaxf(top, sm[group - g + i]);
+      m = top;
+      sum = 0;
+      for (int j = 0; j < 8; ++j) y[j] = 0;
+      for (int i = 0; i < groups; ++i) {
+        const float w = exp2f(sm[group - g + i] - (top == -INFINITY ? 0.0f : top));
+        sum += w * ssum[group - g + i];
+        for (int j = 0; j < 8; ++j) y[j] += w * sy[group - g + i][lane * 8 + j];
+      }
+      __syncthreads();
+    }
+    if (g == 0 && r < all) {
+      const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+      uint32_t w[4];
+      for (int j = 0; j < 4; ++j) w[j] = pack2<TYPE>(y[2 * j] * inv, y[2 * j + 1] * inv);
+      *(u32x4*)(out.p + ((sq.r0 + r / a.heads) * out.row + (r % a.heads) * out.head + lane * 8) * 2) = u32x4{w[0], w[1], w[2], w[3]};
+      if (lse && lane == 0) lse[at] = sum == 0 ? -INFINITY : (m + log2f(sum)) * kLn2;
+    }
   }
 }
 
@@ -50,10 +94,12 @@ AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
   // tiles that the longest sequence's last block sees
   const long seen = a.window ? std::min<long>(a.max_len, (long)a.window + per_block / a.G + a.sinks + 2 * tile) : a.max_len;
   const long tiles = (seen + tile - 1) / tile, groups = (long)B * c.H * p.blocks;
-  const long fill = p.tile ? (p.nb == 4 ? 2 : 1) * device_cus() : 2 * device_cus();
-  long splits = forced_splits ? forced_splits : std::min(std::max<long>(1, fill / groups), std::max<long>(1, tiles / 8));
+  const long fill = p.tile ? (p.nb == 4 ? 2 : 1) * device_cus() : device_cus();
+  const long unit = p.tile ? 1 : rows_waves(p.nb), least = p.tile ? 8 : unit;
+  long splits = forced_splits ? forced_splits : std::min(std::max<long>(1, fill / groups), std::max<long>(1, tiles / least));
+  if (!forced_splits && !p.tile) splits = std::max(splits, tiles * 32 / 8192);
   long per = (tiles + splits - 1) / splits;
-  if (!p.tile) per = (per + 3) / 4 * 4;
+  per = (per + unit - 1) / unit * unit;
   p.per_split = (int)per;
   p.splits = (int)((tiles + per - 1) / per);
   return p;
@@ -61,7 +107,7 @@ AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
 
 }  // namespace
 
-size_t partial_bytes(const AttendPlan& p, const KvCache& c, const Attend& a, int rows) {
+static size_t partial_bytes(const AttendPlan& p, const KvCache& c, const Attend& a, int rows) {
   return p.splits > 1 ? (size_t)p.splits * rows * a.heads * (c.D + 1) * sizeof(float) : 0;
 }
 
@@ -74,15 +120,18 @@ int launch_attend(const KvCache& c, const KvBatch& b, const Attend& a, const Den
   const AttendPlan p = attend_plan(c, a, b.B, b.rows);
   Partial part = {(float*)workspace, nullptr, (long)b.rows * a.heads};
   part.lse = part.o + p.splits * part.rows * c.D;
-  (p.tile ? launch_attend_tile : launch_attend_rows)(p, c, b, a, q, out, lse, part, s);
+  const AttendArgs args = {c, b, a, p.splits, p.per_split, q, out, lse, part};
+  (p.tile ? launch_attend_tile : launch_attend_rows)(p, args, s);
   int st = check_launch("attend");
   if (st || p.splits == 1) return st;
-  const long per_seq = (long)std::min(a.max_rows, b.rows) * a.heads * (c.D / 8);
-  const dim3 grid((unsigned)std::min<long>((per_seq + 255) / 256, 1 << 20), 1, b.B);
+  int groups = 1;
+  while (groups < 16 && groups * 2 <= p.splits) groups *= 2;
+  const long per_block = kJoinThreads / (c.D / 8) / groups, per_seq = (long)std::min(a.max_rows, b.rows) * a.heads;
+  const dim3 grid((unsigned)std::min<long>((per_seq + per_block - 1) / per_block, 1 << 20), 1, b.B);
   auto go = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (a.type == GRINQH_F16) k_attend_join<D, GRINQH_F16><<<grid, 256, 0, s>>>(c, b, a, out, lse, part, p.splits);
-    else k_attend_join<D, GRINQH_BF16><<<grid, 256, 0, s>>>(c, b, a, out, lse, part, p.splits);
+    if (a.type == GRINQH_F16) k_attend_join<D, GRINQH_F16><<<grid, kJoinThreads, 0, s>>>(c, b, a, out, lse, part, p.splits, groups);
+    else k_attend_join<D, GRINQH_BF16><<<grid, kJoinThreads, 0, s>>>(c, b, a, out, lse, part, p.splits, groups);
   };
   if (c.D == 64) go(std::integral_constant<int, 64>{});
   else go(std::integral_constant<int, 128>{});

@@ -9,6 +9,8 @@
 //   - a lane loads D / 16 consecutive values of each of those 8 tokens of V; byte permutes turn the 8 x D / 16
 //     block round into D / 16 operands whose row is the channel (D / 16) (lane % 16) + j.
 //   - int8 codes become fp16 on the way (exact); K's scales multiply the scores, V's the weights.
+//   - pages of 16 tokens or more hold a block whole: its address is scalar, the lanes' offsets are constant.
+//     Smaller pages (SMALL) pass the 32 tokens' addresses and scales through LDS.
 // The next tile's K is loaded while the softmax runs, its V behind the second product.
 #include "attend.h"
 
@@ -16,20 +18,16 @@ namespace grinqh {
 
 namespace {
 
-constexpr int kWaves = 4;
 constexpr int kTile = 32;
 
-// What a token that is not there reads: zeros past the last token, NaN for a page id out of range.
-__device__ const uint32_t g_filler[2][64] = {
-    {0},
-    {0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-     0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-     0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-     0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-     0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-     0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-     0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-     0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff}};
+// What is read for tokens that are not there, a block of 16 rows each: zeros behind the last token, NaN for K of a page
+// id out of range.  (A scale reads the first words.)
+constexpr int kFill = 16 * 256 / 4;
+__device__ const uint32_t g_zeros[kFill] = {0};
+#define NAN4 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff
+#define NAN64 NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4
+__device__ const uint32_t g_nans[kFill] = {NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64,
+                                           NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64};
 
 // What a value that is not finite adds where it is seen: 1 in the halves of w that are +inf or NaN
 // (sign = 0), -inf or NaN (sign = 1).
@@ -60,11 +58,11 @@ struct alignas(16) WaveTokens {
   float vs[kTile];
 };
 
-template <int D, int NB>
+template <int D, int NB, int WAVES>
 struct RowsLds {
-  WaveTokens tokens[kWaves];
-  float m[kWaves][16 * NB], l[kWaves][16 * NB];
-  float o[kWaves][16][D + 4];   // one block of 16 rows at a time
+  WaveTokens tokens[WAVES];
+  float m[WAVES][16 * NB], l[WAVES][16 * NB];
+  float o[WAVES][16][D + 4];   // one block of 16 rows at a time
 };
 
 template <int W>
@@ -73,24 +71,30 @@ struct Words { uint32_t w[W]; };
 template <int W>
 __device__ __forceinline__ Words<W> load_words(const char* p) {
   Words<W> r;
-  if constexpr (W == 1) r.w[0] = *(const uint32_t*)p;
-  else if constexpr (W == 2) { const u32x2 x = *(const u32x2*)p; r.w[0] = x[0]; r.w[1] = x[1]; }
-  else { const u32x4 x = *(const u32x4*)p; for (int i = 0; i < 4; ++i) r.w[i] = x[i]; }
+  if constexpr (W == 1) r.w[0] = load_global<uint32_t>(p);
+  else if constexpr (W == 2) { const u32x2 x = load_global<u32x2>(p); r.w[0] = x[0]; r.w[1] = x[1]; }
+  else { const u32x4 x = load_global<u32x4>(p); for (int i = 0; i < 4; ++i) r.w[i] = x[i]; }
   return r;
 }
 
-template <int D, int FORMAT, int TYPE, int NB>
-__global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out,
-                                                             float* lse, Partial part, int splits, int per_split) {
+template <int D, int FORMAT, int TYPE, int NB, bool SMALL>
+__global__ __launch_bounds__(64 * rows_waves(NB)) __attribute__((amdgpu_waves_per_eu(rows_per_simd(FORMAT, NB))))
+void k_attend_rows(AttendArgs args) {
+  const KvCache& c = args.c;
+  const KvBatch& b = args.b;
+  const Attend& a = args.a;
+  const int splits = args.splits, per_split = args.per_split;
   constexpr bool I8 = FORMAT == GRINQH_KV_I8;
   constexpr int ES = I8 ? 1 : 2;             // bytes of a cached value
   constexpr int KS = D / 32;                 // steps of the first product
   constexpr int KL = I8 ? D / 64 : D / 32;   // 16-byte loads of a K row per lane
   constexpr int VC = D / 16;                 // channels of V per lane, blocks of the second product
   constexpr int VW = VC * ES / 4;            // dwords of those
-  __shared__ RowsLds<D, NB> lds;
+  constexpr int WAVES = rows_waves(NB);
+  __shared__ RowsLds<D, NB, WAVES> lds;
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, quad = lane >> 4;
+  const int lane = threadIdx.x & 63, i16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int h = blockIdx.x % c.H, split = blockIdx.x / c.H, s = blockIdx.z;
   const Seq sq = kv_seq(c, b, s);
   const int all = sq.n * a.G;                // rows of this kv head
@@ -103,16 +107,16 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
     const int v0 = split * per_split + wave;
 
     // this lane's rows and their queries
-    int pos[NB], row[NB], head[NB];
+    const DenseRows q = late().q;
+    int pos[NB], behind[NB];
     float factor[NB];
     u32x4 qf[NB][KS];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const int r = min(r0 + 16 * n + i16, all - 1);   // rows past the last repeat it and are not stored
-      row[n] = sq.r0 + r / a.G;
-      head[n] = h * a.G + r % a.G;
       pos[n] = sq.L - sq.n + r / a.G;
-      const char* qp = q.p + (row[n] * q.row + head[n] * q.head) * 2;
+      behind[n] = behind_window(a, pos[n]);
+      const char* qp = q.p + ((sq.r0 + r / a.G) * q.row + (h * a.G + r % a.G) * q.head) * 2;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const int d = I8 ? (k >> 1) * 64 + 16 * quad + 8 * (k & 1) : 32 * k + 8 * quad;
@@ -148,40 +152,74 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
       for (int j = 0; j < VC; ++j) o[n][j] = float4v{0, 0, 0, 0};
     }
 
-    // token lane % 32 of virtual tile v: its page id (kept a tile ahead), then where it lies
+    // ---- where virtual tile v's tokens lie: their page ids a tile ahead, then their addresses
     const int* table = b.table + (long)s * b.width;
-    auto token = [&](int v) { return v < v_end ? span.tile(v) * kTile + (lane & 31) : 0x7fffffff; };
-    auto page_id = [&](int v) { const int t = token(v); return t < span.hi ? table[t >> c.shift] : -1; };
-    float ks = 0, vs = 0;
+    auto start = [&](int v) { return v < v_end ? span.tile(v) * kTile : 0x7fffffc0; };   // its first token
+    // lane's token: of the tile (SMALL), else the first of its block of 16 (lanes 0 and 16 are asked)
+    auto page_id = [&](int v) {
+      const int t = start(v) + (SMALL ? lane & 31 : lane & 16);
+      return t < span.hi ? load_global<int>(table + (t >> c.shift)) : -1;
+    };
+    const char* kp[2];
+    const char* vp[2];
+    const float* ksp[2];
+    const float* vsp[2];
+    float ks1 = 0, vs1 = 0;
     auto locate = [&](int v, int id) {
-      const int t = token(v);
-      const bool in = t < span.hi, ok = in && (unsigned)id < (unsigned)c.n_pages;
-      const long slot = ok ? kv_slot(c, id, h, t) : 0;
-      wave_sync();
-      if (lane < 32) {
-        tok.k[lane] = ok ? c.k + slot * D * ES : (const char*)g_filler[in ? 1 : 0];
-        tok.v[lane] = ok ? c.v + slot * D * ES : (const char*)g_filler[0];
+      if constexpr (SMALL) {
+        const int t = start(v) + (lane & 31);
+        const bool in = t < span.hi, ok = in && (unsigned)id < (unsigned)c.n_pages;
+        const long slot = ok ? kv_slot(c, id, h, t) : 0;
+        wave_sync();
+        if (lane < 32) {
+          tok.k[lane] = ok ? c.k + slot * D * ES : (const char*)(in ? g_nans : g_zeros);
+          tok.v[lane] = ok ? c.v + slot * D * ES : (const char*)g_zeros;
+        }
+        if constexpr (I8) {
+          ks1 = load_global<float>(ok ? c.ks + slot : (const float*)(in ? g_nans : g_zeros));
+          vs1 = load_global<float>(ok ? c.vs + slot : (const float*)g_zeros);
+        }
+        wave_sync();
+      } else {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int t = start(v) + 16 * x, pid = __builtin_amdgcn_readlane(id, 16 * x);
+          const bool in = t < span.hi, ok = in && (unsigned)pid < (unsigned)c.n_pages;
+          const long slot = ok ? kv_slot(c, pid, h, t) : 0;
+          kp[x] = ok ? c.k + slot * (D * ES) : (const char*)(in ? g_nans : g_zeros);
+          vp[x] = ok ? c.v + slot * (D * ES) : (const char*)g_zeros;
+          if constexpr (I8) {
+            ksp[x] = ok ? c.ks + slot : (const float*)(in ? g_nans : g_zeros);
+            vsp[x] = ok ? c.vs + slot : (const float*)g_zeros;
+          }
+        }
       }
-      if constexpr (I8) {
-        const float* filler = (const float*)g_filler[in ? 1 : 0];
-        ks = ok ? c.ks[slot] : *filler;
-        vs = ok ? c.vs[slot] : 0.0f;
-      }
-      wave_sync();
     };
     u32x4 kr[2][KL];
     Words<VW> vr[8];
+    float4v kst[2], vst[2];                  // scales of this lane's tokens 16 t + 4 quad ..+ 3
     auto load_k = [&] {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const char* p = tok.k[16 * t + i16];
+        const char* p = SMALL ? tok.k[16 * t + i16] + 16 * quad : kp[t] + (uint32_t)(i16 * D * ES + 16 * quad);
 #pragma unroll
-        for (int k = 0; k < KL; ++k) kr[t][k] = *(const u32x4*)(p + 64 * k + 16 * quad);
+        for (int k = 0; k < KL; ++k) kr[t][k] = load_global<u32x4>(p + 64 * k);
       }
     };
     auto load_v = [&] {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) vr[j] = load_words<VW>(tok.v[(j & 4) * 4 + 4 * quad + (j & 3)] + i16 * VC * ES);
+      for (int j = 0; j < 8; ++j) {
+        const int tk = 4 * quad + (j & 3);
+        const char* p = SMALL ? tok.v[4 * (j & 4) + tk] + i16 * VC * ES : vp[j >> 2] + (uint32_t)((4 * quad * D + i16 * VC) * ES);
+        vr[j] = load_words<VW>(p + (SMALL ? 0 : (j & 3) * D * ES));
+      }
+      if constexpr (I8 && !SMALL) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          kst[t] = load_global<float4v>((const char*)ksp[t] + (uint32_t)(16 * quad));
+          vst[t] = load_global<float4v>((const char*)vsp[t] + (uint32_t)(16 * quad));
+        }
+      }
     };
 
     if (v0 < v_end) {
@@ -189,18 +227,15 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
       load_k();
       load_v();
     }
-    int next_id = page_id(v0 + kWaves);
-    for (int v = v0; v < v_end; v += kWaves) {
+    int next_id = page_id(v0 + WAVES);
+#pragma unroll 1
+    for (int v = v0; v < v_end; v += WAVES) {
       // ---- S^T = K Q^T
       float4v sc[NB][2];
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+      for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          sc[n][t] = float4v{0, 0, 0, 0};
-        }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int n = 0; n < NB; ++n) sc[n][t] = float4v{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           u32x4 f;
@@ -214,54 +249,53 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
 #pragma unroll
           for (int n = 0; n < NB; ++n) sc[n][t] = mfma16<I8 ? GRINQH_KV_F16 : FORMAT>(f, qf[n][k], sc[n][t]);
         }
-      // ---- this tile's scales, then the next tile's K
-      float kst[2][4], vst[2][4];
-      if constexpr (I8) {
+      }
+      if constexpr (I8 && SMALL) {
         wave_sync();
-        if (lane < 32) { tok.ks[lane] = ks; tok.vs[lane] = vs; }
+        if (lane < 32) { tok.ks[lane] = ks1; tok.vs[lane] = vs1; }
         wave_sync();
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const float4v kk = *(const float4v*)&tok.ks[16 * t + 4 * quad], vv = *(const float4v*)&tok.vs[16 * t + 4 * quad];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { kst[t][e] = kk[e]; vst[t][e] = vv[e]; }
+          kst[t] = *(const float4v*)&tok.ks[16 * t + 4 * quad];
+          vst[t] = *(const float4v*)&tok.vs[16 * t + 4 * quad];
         }
       }
-      const int t0 = span.tile(v) * kTile;
-      const bool whole = all_visible(a, first, last, t0, kTile);
-      locate(v + kWaves, next_id);
+      const int t0 = start(v);
+      const bool masked = !all_visible(a, first, last, t0, kTile);
+      // ---- the next tile's K
+      locate(v + WAVES, next_id);
       load_k();
-      next_id = page_id(v + 2 * kWaves);
+      next_id = page_id(v + 2 * WAVES);
       // ---- softmax
-      u32x4 pf[NB], seen[NB];
+      u32x4 pf[NB];
+      uint32_t vis[NB];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        bool vis[2][4];
+        vis[n] = 0xffu;
+        float vmax = 0;
+        if constexpr (I8) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) sc[n][t] *= kst[t];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) vmax = fmaxf(vmax, vst[e >> 2][e & 3]);
+        }
+        if (masked) {
+          vis[n] = 0;
+          vmax = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int tk = t0 + 16 * (e >> 2) + 4 * quad + (e & 3);
+            const bool see = row_sees(tk, pos[n], behind[n], a.sinks);
+            vis[n] |= see ? 1u << e : 0u;
+            sc[n][e >> 2][e & 3] = see ? sc[n][e >> 2][e & 3] : -INFINITY;
+            if constexpr (I8) vmax = fmaxf(vmax, see ? vst[e >> 2][e & 3] : 0.0f);
+          }
+        }
         float mx = -INFINITY;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = sc[n][t][e];
-            if constexpr (I8) x *= kst[t][e];
-            if (!whole) {
-              const int tk = t0 + 16 * t + 4 * quad + e;
-              vis[t][e] = tk <= pos[n] && (!a.window || tk > pos[n] - a.window || tk < a.sinks);
-              if (!vis[t][e]) x = -INFINITY;
-            }
-            sc[n][t][e] = x;
-            mx = fmaxf(mx, x);
-          }
+        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, sc[n][e >> 2][e & 3]);
         mx = max_xor16(max_xor32(mx)) * factor[n];
-        int big = kLowestExponent;
-        if constexpr (I8) {
-          float vmax = 0;
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vmax = fmaxf(vmax, (whole || vis[t][e]) && vst[t][e] < INFINITY ? vst[t][e] : 0.0f);
-          big = scale_exponent(max_xor16(max_xor32(vmax)));
-        }
+        const int big = I8 ? scale_exponent(max_xor16(max_xor32(vmax))) : kLowestExponent;
         // what a row is held against follows its own scores and values alone: other rows, and what
         // they see, never change its bits
         const bool rises = mx > m[n] + kSlack, grows = I8 && big > ev[n];
@@ -276,38 +310,30 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
         const float base = m[n] == -INFINITY ? 0.0f : m[n], down = I8 ? ldexpf(1.0f, kUp - ev[n]) : 1.0f;
         float p[8];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(sc[n][e >> 2][e & 3], factor[n], -base));
+          l[n] += p[e];
+          if constexpr (I8) p[e] *= vst[e >> 2][e & 3] * down;
+        }
+        if constexpr (I8) {
+          if (masked) {   // a scale that is not finite stays with the rows that see it
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = __builtin_amdgcn_exp2f(fmaf(sc[n][t][e], factor[n], -base));
-            l[n] += x;
-            if constexpr (I8) {
-              x *= vst[t][e] * down;
-              if (!whole && !vis[t][e]) x = 0;   // a scale that is not finite stays with the rows that see it
-            }
-            p[4 * t + e] = x;
-          }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pf[n][e] = pack2<FORMAT == GRINQH_KV_BF16 ? GRINQH_BF16 : GRINQH_F16>(p[2 * e], p[2 * e + 1]);
-        if constexpr (!I8) {
-          if (!whole) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              constexpr uint32_t one = FORMAT == GRINQH_KV_F16 ? 0x3c00u : 0x3f80u;
-              seen[n][e] = (vis[e >> 1][2 * (e & 1)] ? one : 0u) | (vis[e >> 1][2 * (e & 1) + 1] ? one << 16 : 0u);
-            }
+            for (int e = 0; e < 8; ++e) p[e] = vis[n] >> e & 1 ? p[e] : 0.0f;
           }
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pf[n][e] = pack2<FORMAT == GRINQH_KV_BF16 ? GRINQH_BF16 : GRINQH_F16>(p[2 * e], p[2 * e + 1]);
       }
       // ---- O^T += V^T P^T
       bool odd = false;   // values that are not finite, in a tile that not all rows see whole
       if constexpr (!I8) {
-        if (!whole) {
-          uint32_t any = 0;
+        if (masked) {
+          uint32_t top = 0;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            for (int w = 0; w < VW; ++w) any |= not_finite<FORMAT>(vr[j].w[w]);
-          odd = __any(any != 0);
+#pragma unroll
+            for (int w = 0; w < VW; ++w) top = max_halves(top, vr[j].w[w] & 0x7fff7fffu);
+          odd = __any(not_finite<FORMAT>(top) != 0);
         }
       }
 #pragma unroll
@@ -325,15 +351,13 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
             f[e] = __builtin_amdgcn_perm(vr[2 * e + 1].w[j >> 1], vr[2 * e].w[j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
           }
         }
-        if constexpr (I8) {
+        if (I8 || !odd) {
 #pragma unroll
-          for (int n = 0; n < NB; ++n) o[n][j] = mfma16<GRINQH_KV_F16>(f, pf[n], o[n][j]);
-        } else if (!odd) {
-#pragma unroll
-          for (int n = 0; n < NB; ++n) o[n][j] = mfma16<FORMAT>(f, pf[n], o[n][j]);
-        } else {
+          for (int n = 0; n < NB; ++n) o[n][j] = mfma16<I8 ? GRINQH_KV_F16 : FORMAT>(f, pf[n], o[n][j]);
+        } else if constexpr (!I8) {
           // 0 times an infinity must not reach rows that do not see it: the finite values as ever, then
           // how many infinities of either sign (a NaN counts as both) a row sees
+          constexpr uint32_t one = FORMAT == GRINQH_KV_F16 ? 0x3c00u : 0x3f80u;
           u32x4 fine, inf[2];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -343,10 +367,13 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
           }
 #pragma unroll
           for (int n = 0; n < NB; ++n) {
+            u32x4 seen;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) seen[e] = (vis[n] >> (2 * e) & 1 ? one : 0u) | (vis[n] >> (2 * e) & 2 ? one << 16 : 0u);
             o[n][j] = mfma16<FORMAT>(fine, pf[n], o[n][j]);
 #pragma unroll
             for (int sign = 0; sign < 2; ++sign) {
-              const float4v count = mfma16<FORMAT>(inf[sign], seen[n], float4v{0, 0, 0, 0});
+              const float4v count = mfma16<FORMAT>(inf[sign], seen, float4v{0, 0, 0, 0});
 #pragma unroll
               for (int e = 0; e < 4; ++e) o[n][j][e] += count[e] > 0 ? (sign ? -INFINITY : INFINITY) : 0.0f;
             }
@@ -357,6 +384,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
     }
 
     // ---- the waves' results meet
+    const DenseRows out = late().out;
+    const Partial part = late().part;
+    float* lse = late().lse;
     float up[NB];   // what brings the sums over the values back
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -368,7 +398,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
     for (int n = 0; n < NB; ++n) {
       __syncthreads();
       float top = -INFINITY;
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds.m[w][16 * n + i16]);
+      for (int w = 0; w < WAVES; ++w) top = fmaxf(top, lds.m[w][16 * n + i16]);
       const float base = top == -INFINITY ? 0.0f : top, f = exp2f(m[n] - base);   // 0 for a wave that saw nothing; a NaN passes
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -376,20 +406,21 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
         for (int j = 0; j < VC; ++j)
           lds.o[wave][i16][VC * (4 * quad + e) + j] = o[n][j][e] * up[n] * f;
       __syncthreads();
-      // 16 lanes per row, D / 16 channels each
-      const int rr = threadIdx.x / 16, ch = (threadIdx.x % 16) * VC, r = r0 + 16 * n + rr;
-      if (r < all) {
-        float rm = -INFINITY, rl = 0;
-        for (int w = 0; w < kWaves; ++w) rm = fmaxf(rm, lds.m[w][16 * n + rr]);
-        const float rb = rm == -INFINITY ? 0.0f : rm;
-        for (int w = 0; w < kWaves; ++w) rl += lds.l[w][16 * n + rr] * exp2f(lds.m[w][16 * n + rr] - rb);
-        float y[VC];
+      // CH channels of a row per thread
+      constexpr int CH = 16 * D / (64 * WAVES) > 2 ? 16 * D / (64 * WAVES) : 2;
+      const int rr = threadIdx.x / (D / CH), ch = (threadIdx.x % (D / CH)) * CH, r = r0 + 16 * n + rr;
+      if (rr < 16 && r < all) {
+        float rm = -INFINITY, rl = 0, y[CH] = {};
 #pragma unroll
-        for (int j = 0; j < VC; ++j) {
-          float x = 0;
-          for (int w = 0; w < kWaves; ++w) x += lds.o[w][rr][ch + j];
-          y[j] = rl == 0 ? 0.0f : x / rl;
+        for (int w = 0; w < WAVES; ++w) rm = fmaxf(rm, lds.m[w][16 * n + rr]);
+        const float rb = rm == -INFINITY ? 0.0f : rm;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+          rl += lds.l[w][16 * n + rr] * exp2f(lds.m[w][16 * n + rr] - rb);
+#pragma unroll
+          for (int j = 0; j < CH; ++j) y[j] += lds.o[w][rr][ch + j];
         }
+        const float inv = rl == 0 ? 0.0f : 1.0f / rl;
         const int rw = sq.r0 + r / a.G, hd = h * a.G + r % a.G;
         const long at = (long)rw * a.heads + hd;
         const float lse2 = rl == 0 ? -INFINITY : rm + log2f(rl);
@@ -398,16 +429,13 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
           if (lse2 != -INFINITY) {
             float* p = part.o + (split * part.rows + at) * D + ch;
 #pragma unroll
-            for (int j = 0; j < VC; j += 4) *(float4v*)(p + j) = float4v{y[j], y[j + 1], y[j + 2], y[j + 3]};
+            for (int j = 0; j < CH; ++j) p[j] = y[j] * inv;
           }
         } else {
           if (lse && ch == 0) lse[at] = lse2 * kLn2;
-          char* p = out.p + (rw * out.row + hd * out.head + ch) * 2;
-          uint32_t w[VC / 2];
+          uint32_t* p = (uint32_t*)(out.p + (rw * out.row + hd * out.head + ch) * 2);
 #pragma unroll
-          for (int j = 0; j < VC / 2; ++j) w[j] = pack2<TYPE>(y[2 * j], y[2 * j + 1]);
-          if constexpr (VC == 8) *(u32x4*)p = u32x4{w[0], w[1], w[2], w[3]};
-          else *(u32x2*)p = u32x2{w[0], w[1]};
+          for (int j = 0; j < CH / 2; ++j) p[j] = pack2<TYPE>(y[2 * j] * inv, y[2 * j + 1] * inv);
         }
       }
     }
@@ -416,25 +444,33 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend_rows(KvCache c, KvBatch 
 }
 
 template <int D, int FORMAT, int TYPE>
-void go(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q, const DenseRows& out,
-        float* lse, const Partial& part, hipStream_t s) {
-  const dim3 grid(c.H * p.splits, p.blocks, b.B);
-  if (p.nb == 1) k_attend_rows<D, FORMAT, TYPE, 1><<<grid, 64 * kWaves, 0, s>>>(c, b, a, q, out, lse, part, p.splits, p.per_split);
-  else k_attend_rows<D, FORMAT, TYPE, 2><<<grid, 64 * kWaves, 0, s>>>(c, b, a, q, out, lse, part, p.splits, p.per_split);
+void go(const AttendPlan& p, const AttendArgs& args, hipStream_t s) {
+  const dim3 grid(args.c.H * p.splits, p.blocks, args.b.B);
+  auto run = [&](auto nb, auto small) {
+    constexpr int NB = decltype(nb)::value;
+    k_attend_rows<D, FORMAT, TYPE, NB, decltype(small)::value>
+        <<<grid, 64 * rows_waves(NB), 0, s>>>(args);
+  };
+  if (args.c.shift >= 4) {
+    if (p.nb == 1) run(std::integral_constant<int, 1>{}, std::false_type{});
+    else run(std::integral_constant<int, 2>{}, std::false_type{});
+  } else {
+    if (p.nb == 1) run(std::integral_constant<int, 1>{}, std::true_type{});
+    else run(std::integral_constant<int, 2>{}, std::true_type{});
+  }
 }
 
 }  // namespace
 
-void launch_attend_rows(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q,
-                        const DenseRows& out, float* lse, const Partial& part, hipStream_t s) {
+void launch_attend_rows(const AttendPlan& p, const AttendArgs& args, hipStream_t s) {
   auto on = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (c.format == GRINQH_KV_F16) go<D, GRINQH_KV_F16, GRINQH_F16>(p, c, b, a, q, out, lse, part, s);
-    else if (c.format == GRINQH_KV_BF16) go<D, GRINQH_KV_BF16, GRINQH_BF16>(p, c, b, a, q, out, lse, part, s);
-    else if (a.type == GRINQH_F16) go<D, GRINQH_KV_I8, GRINQH_F16>(p, c, b, a, q, out, lse, part, s);
-    else go<D, GRINQH_KV_I8, GRINQH_BF16>(p, c, b, a, q, out, lse, part, s);
+    if (args.c.format == GRINQH_KV_F16) go<D, GRINQH_KV_F16, GRINQH_F16>(p, args, s);
+    else if (args.c.format == GRINQH_KV_BF16) go<D, GRINQH_KV_BF16, GRINQH_BF16>(p, args, s);
+    else if (args.a.type == GRINQH_F16) go<D, GRINQH_KV_I8, GRINQH_F16>(p, args, s);
+    else go<D, GRINQH_KV_I8, GRINQH_BF16>(p, args, s);
   };
-  if (c.D == 64) on(std::integral_constant<int, 64>{});
+  if (args.c.D == 64) on(std::integral_constant<int, 64>{});
   else on(std::integral_constant<int, 128>{});
 }
 

@@ -66,8 +66,11 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 
 template <int D, int FORMAT, int TYPE, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, float* lse, Partial part, int splits,
-                   int per_split) {
+void k_attend_tile(AttendArgs args) {
+  const KvCache& c = args.c;
+  const KvBatch& b = args.b;
+  const Attend& a = args.a;
+  const int splits = args.splits, per_split = args.per_split;
   constexpr bool I8 = FORMAT == GRINQH_KV_I8;
   constexpr int MF = I8 ? GRINQH_KV_F16 : FORMAT;   // type of the products
   constexpr int RB = 2 * D;                         // bytes of a row in LDS
@@ -84,8 +87,10 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
   const int* table = b.table + (long)s * b.width;
 
   for (int block = blockIdx.y; block < blocks; block += gridDim.y) {
-    // the last rows see the most tokens: they start first
-    const int r0 = (blocks - 1 - block) * 32 * NW;
+    // the last rows see the most tokens: they start first, and with two workgroups per CU the lightest join
+    // the heaviest
+    const int order = block < (blocks + 1) / 2 || gridDim.z * gridDim.y * gridDim.x > 512 ? blocks - 1 - block : block - (blocks + 1) / 2;
+    const int r0 = order * 32 * NW;
     const int first = sq.L - sq.n + r0 / a.G, last = sq.L - sq.n + min(r0 + 32 * NW - 1, all - 1) / a.G;
     const Span span = attend_span<kTile>(a, first, last);
     const int v0 = split * per_split;
@@ -94,10 +99,12 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
     // this lane's row (both halves of the wave have the same 32), and the span of the wave's rows
     const int w0 = r0 + 32 * wave, r = min(w0 + (lane & 31), all - 1);
     const int row = sq.r0 + r / a.G, head = h * a.G + r % a.G, pos = sq.L - sq.n + r / a.G;
+    const int behind = behind_window(a, pos);
     const int wfirst = __builtin_amdgcn_readfirstlane(sq.L - sq.n + min(w0, all - 1) / a.G);
     const int wlast = __builtin_amdgcn_readfirstlane(sq.L - sq.n + min(w0 + 31, all - 1) / a.G);
     const bool idle = w0 >= all;
 
+    const DenseRows q = late().q;
     u32x4 qf[KS];
     float factor = a.scale * kLog2e;
     {
@@ -156,8 +163,8 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
         const char* kp = ok ? c.k + at : (const char*)(in ? g_nans : g_zeros);
         const char* vp = ok ? c.v + at : (const char*)g_zeros;
         if constexpr (I8) {
-          kr[i] = *(const u32x4*)(kp + 16 * (lane % LPR));
-          vr[i] = *(const u32x4*)(vp + 16 * (lane % LPR));
+          kr[i] = load_global<u32x4>(kp + 16 * (lane % LPR));
+          vr[i] = load_global<u32x4>(vp + 16 * (lane % LPR));
         } else {
           const int rw = row_of(i), to = (64 * NW * i + 64 * wave) * 16;
           __builtin_amdgcn_global_load_lds((global_ptr)(kp + 16 * ((lane % LPR) ^ k_swizzle<D>(rw))),
@@ -172,7 +179,7 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
           const bool in = t < span.hi, ok = in && (unsigned)sid < (unsigned)c.n_pages;
           const float* src = wave ? c.vs : c.ks;
           const float* none = (const float*)(in && !wave ? g_nans : g_zeros);
-          sr = *(ok ? src + kv_slot(c, sid, h, t) : none);
+          sr = load_global<float>(ok ? src + kv_slot(c, sid, h, t) : none);
         }
       }
     };
@@ -274,12 +281,12 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
           unroll<16>([&](auto ec) {
             constexpr int e = decltype(ec)::value;
             const int tk = t0 + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3);
-            const bool see = tk <= pos && (!a.window || tk > pos - a.window || tk < a.sinks);
+            const bool see = row_sees(tk, pos, behind, a.sinks);
             vis[t] |= see ? 1u << e : 0u;
             sc[t][e] = see ? sc[t][e] : -INFINITY;
             if constexpr (I8) {
               const float w = bcast16<e>(vst[t]);
-              vmax = fmaxf(vmax, see && w < INFINITY ? w : 0.0f);
+              vmax = fmaxf(vmax, see && w < INFINITY ? w : 0.0f);   // rows share a factor below
             }
           });
         }
@@ -303,9 +310,22 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[j][e] *= alpha;
       }
-      const float base = m == -INFINITY ? 0.0f : m, down = I8 ? ldexpf(1.0f, kUp - ev) : 1.0f;
-      // rows that have seen the same scales share a factor, which then goes into the tokens' scales
-      const bool shared = I8 && __all(ev == __builtin_amdgcn_readfirstlane(ev));
+      const float base = m == -INFINITY ? 0.0f : m;
+      // the factor 2^(kUp - ev) goes into the tokens' scales, which the wave shares: that of the largest ev,
+      // and where rows differ what is left of theirs (powers of two: exact)
+      float down = 1, fix = 1;
+      bool shared = true;
+      if constexpr (I8) {
+        int top = __builtin_amdgcn_readfirstlane(ev);
+        shared = __all(ev == top);
+        if (!shared) {
+          top = ev;
+#pragma unroll
+          for (int x = 1; x < 32; x <<= 1) top = max(top, __shfl_xor(top, x));
+          fix = ldexpf(1.0f, min(top - ev, 127));
+        }
+        down = ldexpf(1.0f, kUp - top);
+      }
       u32x4 pf[2][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -316,17 +336,14 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
           sum += p[e];
         });
         if constexpr (I8) {
-          if (shared) {
-            const float w = vst[t] * down;
-            unroll<16>([&](auto ec) {
-              constexpr int e = decltype(ec)::value;
-              p[e] *= bcast16<e>(w);
-            });
-          } else {
-            unroll<16>([&](auto ec) {
-              constexpr int e = decltype(ec)::value;
-              p[e] *= bcast16<e>(vst[t]) * down;
-            });
+          const float w = vst[t] * down;
+          unroll<16>([&](auto ec) {
+            constexpr int e = decltype(ec)::value;
+            p[e] *= bcast16<e>(w);
+          });
+          if (!shared) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] *= fix;
           }
         }
         if constexpr (I8) {
@@ -380,7 +397,7 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
 #pragma unroll 1
           for (int x = 0; x < kTile; ++x) {
             const int tk = t0 + x;
-            const bool see = tk <= pos && (!a.window || tk > pos - a.window || tk < a.sinks);
+            const bool see = row_sees(tk, pos, behind, a.sinks);
 #pragma unroll
             for (int j = 0; j < VB; ++j)
 #pragma unroll
@@ -424,6 +441,9 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
       }
     }
 
+    const DenseRows out = late().out;
+    const Partial part = late().part;
+    float* lse = late().lse;
     // ---- results: lane = row, 4 channels per quad of registers
     l += __builtin_bit_cast(float, __shfl_xor(__builtin_bit_cast(int, l), 32));
     const float inv = l == 0 ? 0.0f : (I8 ? ldexpf(1.0f, ev - kUp) : 1.0f) / l;
@@ -456,25 +476,23 @@ void k_attend_tile(KvCache c, KvBatch b, Attend a, DenseRows q, DenseRows out, f
 }
 
 template <int D, int FORMAT, int TYPE>
-void go(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q, const DenseRows& out,
-        float* lse, const Partial& part, hipStream_t s) {
-  const dim3 grid(c.H * p.splits, p.blocks, b.B);
-  if (p.nb == 4) k_attend_tile<D, FORMAT, TYPE, 4><<<grid, 256, 0, s>>>(c, b, a, q, out, lse, part, p.splits, p.per_split);
-  else k_attend_tile<D, FORMAT, TYPE, 8><<<grid, 512, 0, s>>>(c, b, a, q, out, lse, part, p.splits, p.per_split);
+void go(const AttendPlan& p, const AttendArgs& args, hipStream_t s) {
+  const dim3 grid(args.c.H * p.splits, p.blocks, args.b.B);
+  if (p.nb == 4) k_attend_tile<D, FORMAT, TYPE, 4><<<grid, 256, 0, s>>>(args);
+  else k_attend_tile<D, FORMAT, TYPE, 8><<<grid, 512, 0, s>>>(args);
 }
 
 }  // namespace
 
-void launch_attend_tile(const AttendPlan& p, const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q,
-                        const DenseRows& out, float* lse, const Partial& part, hipStream_t s) {
+void launch_attend_tile(const AttendPlan& p, const AttendArgs& args, hipStream_t s) {
   auto on = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (c.format == GRINQH_KV_F16) go<D, GRINQH_KV_F16, GRINQH_F16>(p, c, b, a, q, out, lse, part, s);
-    else if (c.format == GRINQH_KV_BF16) go<D, GRINQH_KV_BF16, GRINQH_BF16>(p, c, b, a, q, out, lse, part, s);
-    else if (a.type == GRINQH_F16) go<D, GRINQH_KV_I8, GRINQH_F16>(p, c, b, a, q, out, lse, part, s);
-    else go<D, GRINQH_KV_I8, GRINQH_BF16>(p, c, b, a, q, out, lse, part, s);
+    if (args.c.format == GRINQH_KV_F16) go<D, GRINQH_KV_F16, GRINQH_F16>(p, args, s);
+    else if (args.c.format == GRINQH_KV_BF16) go<D, GRINQH_KV_BF16, GRINQH_BF16>(p, args, s);
+    else if (args.a.type == GRINQH_F16) go<D, GRINQH_KV_I8, GRINQH_F16>(p, args, s);
+    else go<D, GRINQH_KV_I8, GRINQH_BF16>(p, args, s);
   };
-  if (c.D == 64) on(std::integral_constant<int, 64>{});
+  if (args.c.D == 64) on(std::integral_constant<int, 64>{});
   else on(std::integral_constant<int, 128>{});
 }
 

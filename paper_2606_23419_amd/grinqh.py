@@ -105,9 +105,14 @@ class _Rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
-# The arrays of a cache and of a batch, as grinqh.h lays them out.
-KvCache = collections.namedtuple("KvCache", "k v k_scale v_scale")
-KvBatch = collections.namedtuple("KvBatch", "block_table seq_lens row_offsets")
+# The arrays of a cache and of a batch, as grinqh.h lays them out.  They keep the C structure made of them, which is
+# used again as long as it was checked against the same descriptor and every array is where it was.
+class KvCache(collections.namedtuple("KvCache", "k v k_scale v_scale")):
+    pass
+
+
+class KvBatch(collections.namedtuple("KvBatch", "block_table seq_lens row_offsets")):
+    pass
 
 
 def _load():
@@ -541,6 +546,11 @@ def kv_cache(desc: KvDesc, device="cuda") -> KvCache:
 
 
 def _cache_args(desc, cache):
+    at = [t.data_ptr() if t is not None else None for t in cache]
+    key = (desc.format, desc.heads, desc.head_dim, desc.page, desc.n_pages, at)
+    kept = cache.__dict__.get("_args")
+    if kept is not None and kept[0] == key:
+        return kept[1]
     torch = _torch()
     grinqh_kv_bytes(desc)   # validates, so the shapes below mean something
     shape = (desc.n_pages, desc.heads, desc.page)
@@ -551,17 +561,24 @@ def _cache_args(desc, cache):
         t = getattr(cache, n)
         if t is not None:
             setattr(c, n, _dev(t, torch.float32, "cache." + n, shape))
+    cache._args = (key, c)
     return c
 
 
 def _batch_args(batch, rows):
+    key = (int(rows), batch.block_table.data_ptr(), batch.seq_lens.data_ptr(), batch.row_offsets.data_ptr())
+    kept = batch.__dict__.get("_args")
+    if kept is not None and kept[0] == key:
+        return kept[1]
     torch = _torch()
     if batch.seq_lens.dim() != 1 or batch.block_table.dim() != 2:
         raise ValueError("seq_lens must have one axis and block_table two")
     B, width = int(batch.seq_lens.shape[0]), int(batch.block_table.shape[1])
-    return _KvBatch(_dev(batch.block_table, torch.int32, "block_table", (B, width)),
-                    _dev(batch.seq_lens, torch.int32, "seq_lens"),
-                    _dev(batch.row_offsets, torch.int32, "row_offsets", (B + 1,)), B, width, int(rows))
+    b = _KvBatch(_dev(batch.block_table, torch.int32, "block_table", (B, width)),
+                 _dev(batch.seq_lens, torch.int32, "seq_lens"),
+                 _dev(batch.row_offsets, torch.int32, "row_offsets", (B + 1,)), B, width, int(rows))
+    batch._args = (key, b)
+    return b
 
 
 def _rows(t, dtype, name, shape):
