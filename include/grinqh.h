@@ -86,7 +86,7 @@ enum { GRINQH_VMM_ACCUMULATE = 1 };
 enum { GRINQH_OPT_VMM_KERNEL = 1, GRINQH_OPT_GROUPS_PER_WG = 2, GRINQH_OPT_PREFILL_TILE = 3,
        GRINQH_OPT_LUT_GROUPS = 4, GRINQH_OPT_PREFILL_CUS = 5, GRINQH_OPT_ATTEND_KERNEL = 6,
        GRINQH_OPT_ATTEND_SPLITS = 7 };
-enum { GRINQH_ATTEND_ROWS = 1, GRINQH_ATTEND_TILE_4 = 2, GRINQH_ATTEND_TILE_8 = 3 };
+enum { GRINQH_ATTEND_ROWS = 1, GRINQH_ATTEND_TILE = 2 };
 enum { GRINQH_KERNEL_AUTO = 0, GRINQH_KERNEL_PER_PLANE = 1, GRINQH_KERNEL_GENERAL = 2 };
 
 /* Infrastructure, not an operation of the paper.  Fill the auto fields
@@ -407,9 +407,9 @@ GRINQH_API int grinqh_attend(const grinqh_kv_desc* desc, const grinqh_kv_cache* 
  *   GRINQH_OPT_LUT_GROUPS: 1..16 groups per workgroup of the LUT VMM.
  *   GRINQH_OPT_PREFILL_CUS: 1..4096, the CU count the prefill balances its
  *     rounds of 256x256 tiles for (0: the device's).
- *   GRINQH_OPT_ATTEND_KERNEL: GRINQH_ATTEND_ROWS (a few rows per workgroup),
- *     GRINQH_ATTEND_TILE_4 or _8 (128 or 256 rows); GRINQH_OPT_ATTEND_SPLITS:
- *     1..1024 parts of a sequence's tokens.  grinqh_attend_workspace_bytes
+ *   GRINQH_OPT_ATTEND_KERNEL: GRINQH_ATTEND_ROWS (16 or 32 rows per workgroup)
+ *     or GRINQH_ATTEND_TILE (256); GRINQH_OPT_ATTEND_SPLITS: 1..1024 parts of
+ *     a sequence's tokens.  grinqh_attend_workspace_bytes
  *     follows both, so set them before asking for the size.
  * Returns GRINQH_EINVAL for an unknown option or a value out of range.  The
  * setting is read when a call enqueues its kernels; set it between calls. */

@@ -25,7 +25,7 @@ struct Partial {
 // How a call is launched (attend.hip).
 struct AttendPlan {
   bool tile;        // k_attend_tile, else k_attend_rows
-  int nb;           // k_attend_rows: blocks of 16 rows per wave; k_attend_tile: waves of 32 rows
+  int nb;           // k_attend_rows: blocks of 16 rows per wave
   int blocks;       // row blocks of the longest sequence, as far as the caller's estimate goes
   int splits;       // parts of a sequence's tiles, and tiles per part (the last takes the rest)
   int per_split;
@@ -60,6 +60,17 @@ __device__ __forceinline__ const AttendArgs& late() {
 // four waves share a CU, so that one's start and end overlap with the others' loads.
 constexpr int rows_waves(int nb) { return nb == 1 ? 4 : 8; }
 constexpr int rows_per_simd(int format, int nb) { return format == GRINQH_KV_I8 && nb == 1 ? 3 : 2; }
+
+// What is read for tokens that are not there, a block of 16 rows each: zeros behind the last token, NaN for K of a page
+// id out of range.  (A scale reads the first words.)
+constexpr int kFill = 16 * 256 / 4;
+static __device__ const uint32_t g_zeros[kFill] = {0};
+#define NAN4 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff
+#define NAN64 NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4
+static __device__ const uint32_t g_nans[kFill] = {NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64,
+                                           NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64};
+#undef NAN64
+#undef NAN4
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;

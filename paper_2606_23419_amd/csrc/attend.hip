@@ -88,13 +88,13 @@ AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
   const int forced = option(&Options::attend_kernel), forced_splits = option(&Options::attend_splits);
   const long n = std::min(a.max_rows, rows), R = n * a.G;
   p.tile = forced ? forced != GRINQH_ATTEND_ROWS : R > 32;
-  p.nb = p.tile ? (forced == GRINQH_ATTEND_TILE_4 ? 4 : 8) : R > 16 ? 2 : 1;
-  const long per_block = p.tile ? 32 * p.nb : 16 * p.nb, tile = p.tile ? 64 : 32;
+  p.nb = R > 16 ? 2 : 1;
+  const long per_block = p.tile ? 256 : 16 * p.nb, tile = p.tile ? 64 : 32;
   p.blocks = (int)std::min<long>((R + per_block - 1) / per_block, 65535);
   // tiles that the longest sequence's last block sees
   const long seen = a.window ? std::min<long>(a.max_len, (long)a.window + per_block / a.G + a.sinks + 2 * tile) : a.max_len;
   const long tiles = (seen + tile - 1) / tile, groups = (long)B * c.H * p.blocks;
-  const long fill = p.tile ? (p.nb == 4 ? 2 : 1) * device_cus() : device_cus();
+  const long fill = device_cus();
   const long unit = p.tile ? 1 : rows_waves(p.nb), least = p.tile ? 8 : unit;
   long splits = forced_splits ? forced_splits : std::min(std::max<long>(1, fill / groups), std::max<long>(1, tiles / least));
   if (!forced_splits && !p.tile) splits = std::max(splits, tiles * 32 / 8192);

@@ -20,15 +20,6 @@ namespace {
 
 constexpr int kTile = 32;
 
-// What is read for tokens that are not there, a block of 16 rows each: zeros behind the last token, NaN for K of a page
-// id out of range.  (A scale reads the first words.)
-constexpr int kFill = 16 * 256 / 4;
-__device__ const uint32_t g_zeros[kFill] = {0};
-#define NAN4 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff
-#define NAN64 NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4, NAN4
-__device__ const uint32_t g_nans[kFill] = {NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64,
-                                           NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64, NAN64};
-
 // What a value that is not finite adds where it is seen: 1 in the halves of w that are +inf or NaN
 // (sign = 0), -inf or NaN (sign = 1).
 template <int FORMAT>

@@ -10,7 +10,7 @@
 //   - 16-byte chunks of K's and V's rows are swizzled in LDS so that neither read conflicts.
 // 16-bit rows go to LDS directly; int8 rows pass through registers and become fp16 codes (exact), K's scales
 // multiply the scores and V's the weights, each lane holding the scale of one token that the multiplication
-// broadcasts by DPP.  The next tile's rows are under way while one is multiplied; one barrier per tile.
+// broadcasts by DPP.  Tiles are double-buffered, and the waves run in two halves half a tile apart.
 #include "attend.h"
 
 namespace grinqh {
@@ -18,17 +18,7 @@ namespace grinqh {
 namespace {
 
 constexpr int kTile = 64;
-
-__device__ const uint32_t g_zeros[64] = {0};
-__device__ const uint32_t g_nans[64] = {
-    0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-    0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-    0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-    0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-    0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-    0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-    0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff,
-    0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff};
+constexpr int kWaves = 8;
 
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void unroll(F&& f) {
@@ -51,21 +41,25 @@ __device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 15 :
 template <int D>
 __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? (row & 3) << 2 : (row >> 1 & 1) << 2; }
 
-template <int D>
+// Tiles of fp16 or bf16 rows; an 8-bit cache's codes as they come, and its scales.
+template <int D, bool I8>
 struct TileLds {
-  uint8_t k[2][kTile][2 * D];
-  uint8_t v[2][kTile][2 * D];
-  float ks[2][kTile], vs[2][kTile];
-  int vmax[2];
-  int odd[2][8];     // per wave: what it staged of V holds a value that is not finite
+  static constexpr int kBuffers = I8 ? 3 : 4;
+  uint8_t k[kBuffers][kTile][2 * D];
+  uint8_t v[kBuffers][kTile][2 * D];
+  uint8_t raw_k[I8 ? 2 : 1][I8 ? kTile * D : 16];
+  uint8_t raw_v[I8 ? 2 : 1][I8 ? kTile * D : 16];
+  float ks[4][kTile], vs[4][kTile];
+  int vmax[4];
+  int odd[4][kWaves];   // per wave: what it staged of V held a value that is not finite
 };
 
 typedef const __attribute__((address_space(1))) void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef short short4v __attribute__((ext_vector_type(4)));
 
-template <int D, int FORMAT, int TYPE, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
+template <int D, int FORMAT, int TYPE, bool SMALL>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void k_attend_tile(AttendArgs args) {
   const KvCache& c = args.c;
   const KvBatch& b = args.b;
@@ -76,22 +70,20 @@ void k_attend_tile(AttendArgs args) {
   constexpr int RB = 2 * D;                         // bytes of a row in LDS
   constexpr int ES = I8 ? 1 : 2;
   constexpr int LPR = D * ES / 16;                  // lanes per row of a staged load
-  constexpr int LOADS = kTile * LPR / (64 * NW) > 0 ? kTile * LPR / (64 * NW) : 1;   // per lane, for K and for V
+  constexpr int LOADS = kTile * LPR / (64 * kWaves) > 0 ? kTile * LPR / (64 * kWaves) : 1;   // per lane, for K and for V
   constexpr int KS = D / 16, VB = D / 32;
-  __shared__ __attribute__((aligned(1024))) TileLds<D> lds;
+  __shared__ __attribute__((aligned(1024))) TileLds<D, I8> lds;
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, i16 = lane & 15;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, i16 = lane & 15;
   const int h = blockIdx.x % c.H, split = blockIdx.x / c.H, s = blockIdx.z;
   const Seq sq = kv_seq(c, b, s);
-  const int all = sq.n * a.G, blocks = (all + 32 * NW - 1) / (32 * NW);
+  const int all = sq.n * a.G, blocks = (all + 32 * kWaves - 1) / (32 * kWaves);
   const int* table = b.table + (long)s * b.width;
 
   for (int block = blockIdx.y; block < blocks; block += gridDim.y) {
-    // the last rows see the most tokens: they start first, and with two workgroups per CU the lightest join
-    // the heaviest
-    const int order = block < (blocks + 1) / 2 || gridDim.z * gridDim.y * gridDim.x > 512 ? blocks - 1 - block : block - (blocks + 1) / 2;
-    const int r0 = order * 32 * NW;
-    const int first = sq.L - sq.n + r0 / a.G, last = sq.L - sq.n + min(r0 + 32 * NW - 1, all - 1) / a.G;
+    // the last rows see the most tokens: they start first
+    const int r0 = (blocks - 1 - block) * 32 * kWaves;
+    const int first = sq.L - sq.n + r0 / a.G, last = sq.L - sq.n + min(r0 + 32 * kWaves - 1, all - 1) / a.G;
     const Span span = attend_span<kTile>(a, first, last);
     const int v0 = split * per_split;
     const int v_end = split == splits - 1 ? span.tiles : min(span.tiles, v0 + per_split);
@@ -102,7 +94,6 @@ void k_attend_tile(AttendArgs args) {
     const int behind = behind_window(a, pos);
     const int wfirst = __builtin_amdgcn_readfirstlane(sq.L - sq.n + min(w0, all - 1) / a.G);
     const int wlast = __builtin_amdgcn_readfirstlane(sq.L - sq.n + min(w0 + 31, all - 1) / a.G);
-    const bool idle = w0 >= all;
 
     const DenseRows q = late().q;
     u32x4 qf[KS];
@@ -141,131 +132,235 @@ void k_attend_tile(AttendArgs args) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[j][e] = 0;
 
-    // ---- staging: load i of a lane is chunk lane % LPR of row (64 NW i + thread) / LPR of the tile
-    int ids[LOADS], sid = 0;
-    u32x4 kr[LOADS], vr[LOADS];
-    float sr = 0;
-    const bool stages = LOADS > 1 || (int)threadIdx.x < kTile * LPR;
-    auto token = [&](int v, int t) { return v < v_end ? span.tile(v) * kTile + t : 0x7fffffff; };
-    auto lookup = [&](int v, int t) { const int x = token(v, t); return x < span.hi ? table[x >> c.shift] : -1; };
-    auto row_of = [&](int i) { return (64 * NW * i + (int)threadIdx.x) / LPR; };
-    auto look = [&](int v) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) ids[i] = lookup(v, row_of(i) % kTile);
-      if constexpr (I8) if (wave < 2) sid = lookup(v, lane);
+    // ---- staging: load i of a lane is chunk lane % LPR of row (64 kWaves i + thread) / LPR of the tile.  The rows of
+    // one load of a wave lie in one page of 16 tokens or more: its address is scalar and the lanes' offsets do
+    // not change.  Smaller pages (SMALL) are looked up by the lanes.  Page ids are read a tile ahead.
+    constexpr int RPW = 64 / LPR;            // rows of a load of a wave
+    static_assert(RPW <= 16);
+    const int N = v_end - v0;                // tiles, counted from 0 from here on
+    auto start = [&](int i) { const int v = v0 + i; return i < N ? span.tile(v) * kTile : 0x7fffffc0; };
+    auto first_row = [&](int i) { return (kWaves * i + wave) * RPW % kTile; };
+    const int my_row = lane / LPR, my_chunk = lane % LPR;
+    const bool stages = (kWaves * (LOADS - 1) + wave) * RPW < kTile;   // else it repeats others' rows
+    // byte offset of a load's first row (SMALL: of this lane's) in the arrays, or what is read in its place
+    constexpr long kAbsent = -1, kBad = -2;
+    int id[LOADS];                           // page ids of the next tile of K
+    long at[LOADS];                          // offsets of the last tile of K: V's next
+    int sid[4];                              // page ids of the next tile's scales (SMALL: this lane's)
+    auto page_of = [&](int t) { return t < span.hi ? table[t >> c.shift] : -1; };
+    auto offset_of = [&](int t, int page, int size) {
+      return t >= span.hi ? kAbsent : (unsigned)page >= (unsigned)c.n_pages ? kBad : kv_slot(c, page, h, t) * size;
     };
-    auto fetch = [&](int v, int buf) {
+    auto row_at = [&](int i, int x) { return start(i) + first_row(x) + (SMALL ? my_row : 0); };
+    auto look = [&](int i) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int t = token(v, row_of(i) % kTile);
-        const bool in = t < span.hi, ok = in && (unsigned)ids[i] < (unsigned)c.n_pages;
-        const long at = ok ? kv_slot(c, ids[i], h, t) * (D * ES) : 0;
-        const char* kp = ok ? c.k + at : (const char*)(in ? g_nans : g_zeros);
-        const char* vp = ok ? c.v + at : (const char*)g_zeros;
-        if constexpr (I8) {
-          kr[i] = load_global<u32x4>(kp + 16 * (lane % LPR));
-          vr[i] = load_global<u32x4>(vp + 16 * (lane % LPR));
-        } else {
-          const int rw = row_of(i), to = (64 * NW * i + 64 * wave) * 16;
-          __builtin_amdgcn_global_load_lds((global_ptr)(kp + 16 * ((lane % LPR) ^ k_swizzle<D>(rw))),
-                                           (lds_ptr)(&lds.k[buf][0][0] + to), 16, 0, 0);
-          __builtin_amdgcn_global_load_lds((global_ptr)(vp + 16 * ((lane % LPR) ^ v_swizzle<D>(rw))),
-                                           (lds_ptr)(&lds.v[buf][0][0] + to), 16, 0, 0);
-        }
-      }
+      for (int x = 0; x < LOADS; ++x) id[x] = page_of(row_at(i, x));
       if constexpr (I8) {
         if (wave < 2) {
-          const int t = token(v, lane);
-          const bool in = t < span.hi, ok = in && (unsigned)sid < (unsigned)c.n_pages;
-          const float* src = wave ? c.vs : c.ks;
-          const float* none = (const float*)(in && !wave ? g_nans : g_zeros);
-          sr = load_global<float>(ok ? src + kv_slot(c, sid, h, t) : none);
+#pragma unroll
+          for (int x = 0; x < (SMALL ? 1 : 4); ++x) sid[x] = page_of(start(i) + (SMALL ? lane : 16 * x));
         }
       }
     };
-    // int8 codes as fp16 into LDS
-    auto put = [&](int buf) {
+    // a lane's chunk from there: SMALL adds none for the row
+    uint32_t kat[LOADS], vat[LOADS];
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      const int rw = first_row(x) + my_row, from = SMALL ? 0 : my_row * D * ES;
+      kat[x] = from + 16 * (I8 ? my_chunk : my_chunk ^ k_swizzle<D>(rw));
+      vat[x] = from + 16 * (I8 ? my_chunk : my_chunk ^ v_swizzle<D>(rw));
+    }
+    auto copy = [&](const char* from, uint8_t* to, int x) {
+      if (stages) __builtin_amdgcn_global_load_lds((global_ptr)from, (lds_ptr)(to + (64 * kWaves * x + 64 * wave) * 16), 16, 0, 0);
+    };
+    // V of the tile that at[] stands for, into buffer or raw slot `to`
+    auto fetch_v = [&](int to) {
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x)
+        copy((at[x] >= 0 ? c.v + at[x] : (const char*)g_zeros) + vat[x], I8 ? lds.raw_v[to] : &lds.v[I8 ? 0 : to][0][0], x);
+    };
+    // K of tile i, whose page ids look(i) has read, and its scales
+    auto fetch_k = [&](int i, int to) {
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) {
+        at[x] = offset_of(row_at(i, x), id[x], D * ES);
+        copy((at[x] >= 0 ? c.k + at[x] : (const char*)(at[x] == kBad ? g_nans : g_zeros)) + kat[x],
+             I8 ? lds.raw_k[to] : &lds.k[I8 ? 0 : to][0][0], x);
+      }
       if constexpr (I8) {
-        if (stages) {
+        if (wave < 2) {   // a token per lane
+          const int t = start(i) + lane, page = SMALL ? sid[0] : lane < 32 ? lane < 16 ? sid[0] : sid[1] : lane < 48 ? sid[2] : sid[3];
+          const long o = offset_of(t, page, 4);
+          const char* from = o >= 0 ? (const char*)(wave ? c.vs : c.ks) + o : (const char*)(o == kBad && !wave ? g_nans : g_zeros);
+          __builtin_amdgcn_global_load_lds((global_ptr)from, (lds_ptr)(wave ? lds.vs[i & 3] : lds.ks[i & 3]), 4, 0, 0);
+        }
+      }
+    };
+    // This wave's part of raw codes as fp16 into LDS; its scales' largest exponent.
+    auto convert = [&](const uint8_t* raw, uint8_t (*to)[RB], auto swizzle) {
+      if (stages) {
 #pragma unroll
-          for (int i = 0; i < LOADS; ++i) {
-            const int rw = row_of(i), ch = 2 * (lane % LPR);
+        for (int x = 0; x < LOADS; ++x) {
+          const u32x4 r = *(const u32x4*)(raw + (64 * kWaves * x + (int)threadIdx.x) * 16);
+          const int rw = first_row(x) + my_row, ch = 2 * my_chunk;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              u32x4 kk, vv;
+          for (int y = 0; y < 2; ++y) {
+            u32x4 w;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                kk[e] = codes2(kr[i][2 * x + (e >> 1)] ^ 0x80808080u, 2 * (e & 1), 2 * (e & 1) + 1);
-                vv[e] = codes2(vr[i][2 * x + (e >> 1)] ^ 0x80808080u, 2 * (e & 1), 2 * (e & 1) + 1);
-              }
-              *(u32x4*)&lds.k[buf][rw][16 * ((ch + x) ^ k_swizzle<D>(rw))] = kk;
-              *(u32x4*)&lds.v[buf][rw][16 * ((ch + x) ^ v_swizzle<D>(rw))] = vv;
+            for (int e = 0; e < 4; ++e) w[e] = codes2(r[2 * y + (e >> 1)] ^ 0x80808080u, 2 * (e & 1), 2 * (e & 1) + 1);
+            *(u32x4*)&to[rw][16 * ((ch + y) ^ swizzle(rw))] = w;
+          }
+        }
+      }
+    };
+    auto convert_k = [&](int i, int raw, int to) {
+      convert(lds.raw_k[raw], lds.k[to], [](int rw) { return k_swizzle<D>(rw); });
+      if (wave == 1) {
+        const float sr = lds.vs[i & 3][lane];
+        int big = sr > 0 && sr < INFINITY ? scale_exponent(sr) : kLowestExponent;
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) big = max(big, __shfl_xor(big, x));
+        if (lane == 0) lds.vmax[i & 3] = big;
+      }
+    };
+    auto convert_v = [&](int raw, int to) { convert(lds.raw_v[raw], lds.v[to], [](int rw) { return v_swizzle<D>(rw); }); };
+
+    // Tiles that every row of the workgroup, or of the wave, sees whole: those inside the sinks, and from the last
+    // row's window start to the first row's position.
+    const int inner = a.sinks / kTile, shift_i = span.sink_tiles - span.lo_tile - v0;   // tile of tokens t is i = t / 64 + shift_i
+    auto tiles_from = [&](int p) { return (a.window ? max(p - a.window + 1 + kTile - 1, 0) / kTile : 0) + shift_i; };
+    auto tiles_to = [&](int p) { return max(p + 1, 0) / kTile + shift_i; };
+    const int full_from = max(tiles_from(last), span.sink_tiles - v0), full_to = tiles_to(first);
+    const int wave_from = max(tiles_from(wlast), span.sink_tiles - v0), wave_to = tiles_to(wfirst);
+    const int sinks_to = min(inner, span.sink_tiles) - v0;
+    auto full = [&](int i) { return i < sinks_to || (i >= full_from && i < full_to); };
+
+    // A tile that not all rows see whole: values of this wave's part of V that are not finite are set to zero (and
+    // lds.odd says so), since their products with weights of zero would reach rows that do not see them.
+    auto check = [&](int i, int buf) {
+      if constexpr (!I8) {
+        if (i < N && !full(i)) {
+          uint32_t top = 0;
+          u32x4 w[LOADS];
+#pragma unroll
+          for (int x = 0; x < LOADS; ++x) {
+            w[x] = *(const u32x4*)(&lds.v[buf][0][0] + (64 * kWaves * x + (int)threadIdx.x) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max_halves(top, w[x][e] & 0x7fff7fffu);
+          }
+          const int odd = __any(not_finite<FORMAT>(top) != 0);
+          if (lane == 0) lds.odd[i & 3][wave] = odd;
+          if (odd) {
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[x][e] &= ~not_finite<FORMAT>(w[x][e]);
+              *(u32x4*)(&lds.v[buf][0][0] + (64 * kWaves * x + (int)threadIdx.x) * 16) = w[x];
             }
           }
         }
-        if (wave == 0) lds.ks[buf][lane] = sr;
-        if (wave == 1) {
-          lds.vs[buf][lane] = sr;
-          int big = sr > 0 && sr < INFINITY ? scale_exponent(sr) : kLowestExponent;
-#pragma unroll
-          for (int x = 1; x < 64; x <<= 1) big = max(big, __shfl_xor(big, x));
-          if (lane == 0) lds.vmax[buf] = big;
-        }
       }
     };
 
-    // a tile that not all rows see whole: whether this wave's part of V is finite throughout
-    auto check = [&](int v, int buf) {
-      if constexpr (!I8) {
-        if (v < v_end && !all_visible(a, first, last, span.tile(v) * kTile, kTile)) {
-          uint32_t any = 0;
+    // ---- the work on a tile for the wave's rows: products() on the matrix cores, softmax() beside them
+    float16v sc[2];
+    u32x4 pf[2][2];
+    // values(i) of the tile before and scores of tile i, one step at a time: PS steps of 16 tokens and 64 channels of V
+    // (no accumulator twice in a row), then KS steps of 16 channels of K.  The operands are read AHEAD steps ahead,
+    // which is about LDS's latency, and no further: registers are scarce.
+    constexpr int PS = 2 * VB, AHEAD = 4;
+    auto products = [&](int i, int vbuf, int kbuf, auto values_c, auto scores_c) __attribute__((always_inline)) {
+      constexpr int FROM = decltype(values_c)::value ? 0 : PS, TO = decltype(scores_c)::value ? PS + KS : PS;
+      const uint8_t* kb = &lds.k[kbuf][lane & 31][0];
+      const uint8_t* vb = &lds.v[vbuf][4 * half + (i16 >> 2)][32 * (lane >> 4 & 1) + 8 * (i16 & 3)];
+      u32x4 f[AHEAD + 1][2];
+      auto read = [&](auto step_c) __attribute__((always_inline)) {
+        constexpr int step = decltype(step_c)::value;
 #pragma unroll
-          for (int i = 0; i < LOADS; ++i) {
-            const u32x4 w = *(const u32x4*)(&lds.v[buf][0][0] + (64 * NW * i + (int)threadIdx.x) % (kTile * LPR) * 16);
+        for (int y = 0; y < 2; ++y) {
+          u32x4& to = f[step % (AHEAD + 1)][y];
+          if constexpr (step < PS) {
+            const int j = 2 * (step % (VB / 2)) + y, t = step / (VB / 2), at = 16 * ((4 * j) ^ v_swizzle<D>(i16 >> 2));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) any |= not_finite<FORMAT>(w[e]);
+            for (int x = 0; x < 2; ++x) {
+              const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) short4v*)(vb + (16 * t + 8 * x) * RB + at)));
+              to[2 * x] = w[0]; to[2 * x + 1] = w[1];
+            }
+          } else {
+            to = *(const u32x4*)(kb + 32 * RB * y + 16 * ((2 * (step - PS) + half) ^ k_swizzle<D>(lane & 31)));
           }
-          const int odd = __any(any != 0);
-          if (lane == 0) lds.odd[buf][wave] = odd;
+        }
+      };
+      if constexpr (TO > PS) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[t][e] = 0;
+      }
+      unroll<AHEAD>([&](auto x) { read(std::integral_constant<int, FROM + decltype(x)::value>{}); });
+      __builtin_amdgcn_sched_barrier(0);
+      unroll<TO - FROM>([&](auto x) {
+        constexpr int step = FROM + decltype(x)::value;
+        if constexpr (step + AHEAD < TO) read(std::integral_constant<int, step + AHEAD>{});
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const u32x4 w = f[step % (AHEAD + 1)][y];
+          if constexpr (step < PS) {
+            constexpr int j = 2 * (step % (VB / 2)), t = step / (VB / 2);
+            o[j + y] = mfma32<MF>(w, pf[t >> 1][t & 1], o[j + y]);
+          } else {
+            sc[y] = mfma32<MF>(w, qf[step - PS], sc[y]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (!I8 && FROM == 0) {
+        // 0 times an infinity must not reach rows that do not see it: the products took what check() left, and the
+        // rows that see a token get its other values here, from memory
+        bool odd = false;
+        const int t0 = start(i - 1);
+        if (!full(i - 1))
+          for (int w = 0; w < kWaves; ++w) odd |= lds.odd[(i - 1) & 3][w] != 0;
+        if (__any(odd)) {
+#pragma unroll 1
+          for (int x = 0; x < kTile && t0 + x < span.hi; ++x) {
+            const int id = table[(t0 + x) >> c.shift];
+            if ((unsigned)id >= (unsigned)c.n_pages) continue;
+            const bool see = row_sees(t0 + x, pos, behind, a.sinks);
+            const char* from = c.v + kv_slot(c, id, h, t0 + x) * RB + 8 * half;
+#pragma unroll
+            for (int j = 0; j < VB; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const u32x2 w = load_global<u32x2>(from + 16 * (4 * j + e));   // channels 32 j + 8 e + 4 half .. + 3
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                  const uint16_t u = (uint16_t)(w[n >> 1] >> (16 * (n & 1)));
+                  const float y = FORMAT == GRINQH_KV_F16 ? h2f(u) : bf2f(u);
+                  o[j][4 * e + n] += see && !(fabsf(y) < INFINITY) ? y : 0.0f;
+                }
+              }
+          }
         }
       }
     };
-
-    // ---- one tile for the wave's rows.  masked: some row does not see some token; odd: that tile's V holds a
-    // value that is not finite (16-bit formats).  Branches rather than a second copy of the code: with two,
-    // the 64 registers of o are held twice where they meet.
-    auto compute = [&](int buf, int t0, bool masked, bool odd) __attribute__((always_inline)) {
-      float16v sc[2];
-      const uint8_t* kb = &lds.k[buf][lane & 31][0];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sc[t][e] = 0;
-      u32x4 kf[2][2];
-      auto read_k = [&](int k) __attribute__((always_inline)) {
-        const int at = 16 * ((2 * k + half) ^ k_swizzle<D>(lane & 31));
-#pragma unroll
-        for (int t = 0; t < 2; ++t) kf[k & 1][t] = *(const u32x4*)(kb + 32 * RB * t + at);
-      };
-      read_k(0);
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        if (k + 1 < KS) read_k(k + 1);
-        __builtin_amdgcn_sched_barrier(0);   // one step ahead and no further: registers are scarce
-#pragma unroll
-        for (int t = 0; t < 2; ++t) sc[t] = mfma32<MF>(kf[k & 1][t], qf[k], sc[t]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+    // masked: some row of the wave does not see some token.  Branches rather than a second copy of the code: with
+    // two, the 64 registers of o are held twice where they meet.
+    auto softmax = [&](int i) __attribute__((always_inline)) {
+      const int t0 = start(i);
+      const bool masked = !(i < sinks_to || (i >= wave_from && i < wave_to));
       float kst[2], vst[2];
       int big = kLowestExponent;
       if constexpr (I8) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const int tk = 32 * t + 8 * (i16 >> 2) + 4 * half + (i16 & 3);
-          kst[t] = lds.ks[buf][tk];
-          vst[t] = lds.vs[buf][tk];
+          kst[t] = lds.ks[i & 3][tk];
+          vst[t] = lds.vs[i & 3][tk];
         }
-        big = lds.vmax[buf];
+        big = lds.vmax[i & 3];
         unroll<16>([&](auto ec) {
           constexpr int e = decltype(ec)::value;
           sc[0][e] *= bcast16<e>(kst[0]);
@@ -280,8 +375,7 @@ void k_attend_tile(AttendArgs args) {
           vis[t] = 0;
           unroll<16>([&](auto ec) {
             constexpr int e = decltype(ec)::value;
-            const int tk = t0 + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3);
-            const bool see = row_sees(tk, pos, behind, a.sinks);
+            const bool see = row_sees(t0 + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3), pos, behind, a.sinks);
             vis[t] |= see ? 1u << e : 0u;
             sc[t][e] = see ? sc[t][e] : -INFINITY;
             if constexpr (I8) {
@@ -298,6 +392,7 @@ void k_attend_tile(AttendArgs args) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[t][e]);
       mx = max_xor32(mx) * factor;
+      look(i + 4);   // here: a scalar load among reads of LDS would make every wait for them a wait for all
       // a row's own scores and values alone decide what it is held against
       const bool rises = mx > m + kSlack, grows = I8 && big > ev;
       if (__any(rises || grows)) {
@@ -326,7 +421,6 @@ void k_attend_tile(AttendArgs args) {
         }
         down = ldexpf(1.0f, kUp - top);
       }
-      u32x4 pf[2][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         float p[16], sum = 0;
@@ -345,8 +439,6 @@ void k_attend_tile(AttendArgs args) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) p[e] *= fix;
           }
-        }
-        if constexpr (I8) {
           if (masked) {   // a scale that is not finite stays with the rows that see it
 #pragma unroll
             for (int e = 0; e < 16; ++e) p[e] = vis[t] >> e & 1 ? p[e] : 0.0f;
@@ -356,89 +448,73 @@ void k_attend_tile(AttendArgs args) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) pf[t][e >> 2][e & 3] = pack2<MF == GRINQH_KV_BF16 ? GRINQH_BF16 : GRINQH_F16>(p[2 * e], p[2 * e + 1]);
       }
-      const uint8_t* vb = &lds.v[buf][4 * half + (i16 >> 2)][32 * (lane >> 4 & 1) + 8 * (i16 & 3)];
-      u32x4 vf[2][2];   // two steps of 16 tokens, read two ahead
-      auto read_v = [&](int step) __attribute__((always_inline)) {
-        const int j = step >> 1, at = 16 * ((4 * j) ^ v_swizzle<D>(i16 >> 2));
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int t = 2 * (step & 1) + y;
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) short4v*)(vb + (16 * t + 8 * x) * RB + at)));
-            vf[step & 1][y][2 * x] = w[0]; vf[step & 1][y][2 * x + 1] = w[1];
-          }
-        }
-      };
-      read_v(0);
-#pragma unroll
-      for (int step = 0; step < 2 * VB; ++step) {
-        if (step + 1 < 2 * VB) read_v(step + 1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int j = step >> 1, t = 2 * (step & 1) + y;
-          u32x4 f = vf[step & 1][y];
-          if constexpr (!I8) {
-            if (odd) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) f[e] &= ~not_finite<FORMAT>(f[e]);
-            }
-          }
-          o[j] = mfma32<MF>(f, pf[t >> 1][t & 1], o[j]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if constexpr (!I8) {
-        if (odd) {
-          // 0 times an infinity must not reach rows that do not see it: the products above took the finite
-          // values, and the rows that see a token now get its others
-#pragma unroll 1
-          for (int x = 0; x < kTile; ++x) {
-            const int tk = t0 + x;
-            const bool see = row_sees(tk, pos, behind, a.sinks);
-#pragma unroll
-            for (int j = 0; j < VB; ++j)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                // channels 32 j + 8 e + 4 half .. + 3
-                const u32x2 w = *(const u32x2*)&lds.v[buf][x][16 * ((4 * j + e) ^ v_swizzle<D>(x)) + 8 * half];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const uint16_t u = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-                  const float y = FORMAT == GRINQH_KV_F16 ? h2f(u) : bf2f(u);
-                  o[j][4 * e + i] += see && !(fabsf(y) < INFINITY) ? y : 0.0f;
-                }
-              }
-          }
-        }
-      }
+      // the weights are made here and not, as the compiler would have it, where the products take them
+      asm volatile("" : "+v"(pf[0][0]), "+v"(pf[0][1]), "+v"(pf[1][0]), "+v"(pf[1][1]), "+v"(l));
     };
-
-    if (v0 < v_end) {
-      look(v0);
-      fetch(v0, 0);
-      look(v0 + 1);
-      put(0);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // a barrier does not wait for copies into LDS
-      check(v0, 0);
-      __syncthreads();
-      for (int v = v0; v < v_end; ++v) {
-        const int buf = (v - v0) & 1, t0 = span.tile(v) * kTile;
-        fetch(v + 1, buf ^ 1);   // past the end: fillers, never used
-        look(v + 2);
-        if (!idle && t0 <= wlast && (!a.window || t0 + kTile > wfirst - a.window + 1 || t0 < a.sinks)) {
-          bool odd = false;
-          if (!I8 && !all_visible(a, first, last, t0, kTile))
-            for (int w = 0; w < NW; ++w) odd |= lds.odd[buf][w] != 0;
-          compute(buf, t0, !all_visible(a, wfirst, wlast, t0, kTile), __any(odd));
-        }
-        put(buf ^ 1);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        check(v + 1, buf ^ 1);
-        __syncthreads();
+    // ---- the schedule.  Time runs in slots that end in a barrier.  The waves of the first half take the products of
+    // tile i (its scores, and the values of i - 1) in slot 2 i and softmax(i) in slot 2 i + 1, the others a slot later, so
+    // that on every SIMD one wave's softmax runs beside the other's products.  With softmax(i) a wave asks for its part of K
+    // of i + 3 and V of i + 2, and with its products of i + 2 it sees to it that they are there: four slots, for all
+    // workgroups of an XCD walk the same tokens abreast and wait for them to come from HBM.  16-bit rows take
+    // the buffers of tiles i - 1 and i - 2, last read in slot 2 i - 1; codes pass through a slot of their own and become rows in
+    // three buffers with the products of i + 2.  What is there by the end of slot 2 i + 5 is first read in slot 2 i + 6.
+    // Behind the last tile come fillers.
+    auto wait = [&](bool all) {   // a barrier does not wait for copies into LDS: until those of the last softmax, or none, are left
+      if (all || SMALL) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      else if (!I8) { if constexpr (LOADS == 2) asm volatile("s_waitcnt vmcnt(4)" ::: "memory"); else asm volatile("s_waitcnt vmcnt(2)" ::: "memory"); }
+      else if (wave < 2) asm volatile("s_waitcnt vmcnt(3)" ::: "memory");
+      else asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+    };
+    static_assert(LOADS == 1 || (!I8 && LOADS == 2));
+    auto end_slot = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    if (N > 0) {
+      const bool second = wave >= kWaves / 2;
+      look(0);
+      fetch_k(0, 0);
+      fetch_v(0);
+      look(1);
+      fetch_k(1, 1);
+      look(2);
+      if constexpr (I8) {
+        wait(true);
+        convert_k(0, 0, 0);
+        convert_v(0, 0);
+        convert_k(1, 1, 1);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slots have been read
       }
+      fetch_v(1);
+      fetch_k(2, I8 ? 1 : 2);
+      look(3);
+      if constexpr (!I8) {
+        wait(false);
+        check(0, 0);
+      }
+      end_slot();
+      if (second) end_slot();
+      products(0, 0, 0, std::false_type{}, std::true_type{});
+      end_slot();
+      int b3 = 0;                            // i modulo 3
+#pragma unroll 1
+      for (int i = 0; i < N; ++i) {
+        const int n3 = b3 == 2 ? 0 : b3 + 1, nn3 = 3 - b3 - n3;
+        fetch_v(I8 ? i & 1 : (i + 2) & 3);
+        fetch_k(i + 3, I8 ? i & 1 : (i + 3) & 3);
+        softmax(i);
+        end_slot();
+        if constexpr (I8) products(i + 1, b3, n3, std::true_type{}, std::true_type{});
+        else products(i + 1, i & 3, (i + 1) & 3, std::true_type{}, std::true_type{});
+        wait(false);
+        if constexpr (I8) {
+          convert_k(i + 2, (i + 1) & 1, nn3);
+          convert_v((i + 1) & 1, n3);
+        } else {
+          check(i + 1, (i + 1) & 3);
+        }
+        end_slot();
+        b3 = n3;
+      }
+      if (!second) end_slot();
+      wait(true);
     }
 
     const DenseRows out = late().out;
@@ -478,8 +554,8 @@ void k_attend_tile(AttendArgs args) {
 template <int D, int FORMAT, int TYPE>
 void go(const AttendPlan& p, const AttendArgs& args, hipStream_t s) {
   const dim3 grid(args.c.H * p.splits, p.blocks, args.b.B);
-  if (p.nb == 4) k_attend_tile<D, FORMAT, TYPE, 4><<<grid, 256, 0, s>>>(args);
-  else k_attend_tile<D, FORMAT, TYPE, 8><<<grid, 512, 0, s>>>(args);
+  if (args.c.shift >= 4) k_attend_tile<D, FORMAT, TYPE, false><<<grid, 64 * kWaves, 0, s>>>(args);
+  else k_attend_tile<D, FORMAT, TYPE, true><<<grid, 64 * kWaves, 0, s>>>(args);
 }
 
 }  // namespace

@@ -432,7 +432,7 @@ int grinqh_set_option(int opt, int value) {
     case GRINQH_OPT_PREFILL_TILE: field = &Options::prefill_tile; hi = 3; break;
     case GRINQH_OPT_LUT_GROUPS: field = &Options::lut_groups; hi = 16; break;
     case GRINQH_OPT_PREFILL_CUS: field = &Options::prefill_cus; hi = 4096; break;
-    case GRINQH_OPT_ATTEND_KERNEL: field = &Options::attend_kernel; hi = GRINQH_ATTEND_TILE_8; break;
+    case GRINQH_OPT_ATTEND_KERNEL: field = &Options::attend_kernel; hi = GRINQH_ATTEND_TILE; break;
     case GRINQH_OPT_ATTEND_SPLITS: field = &Options::attend_splits; hi = 1024; break;
     default: return fail(GRINQH_EINVAL, "option=%d is not a known option", opt);
   }

@@ -40,8 +40,7 @@ GRINQH_KV_I8 = 2
 GRINQH_OPT_ATTEND_KERNEL = 6
 GRINQH_OPT_ATTEND_SPLITS = 7
 GRINQH_ATTEND_ROWS = 1
-GRINQH_ATTEND_TILE_4 = 2
-GRINQH_ATTEND_TILE_8 = 3
+GRINQH_ATTEND_TILE = 2
 GRINQH_KERNEL_AUTO = 0
 GRINQH_KERNEL_PER_PLANE = 1
 GRINQH_KERNEL_GENERAL = 2

@@ -272,10 +272,10 @@ def test_attend(g, torch, fmt, type, D, H, G, page, seqs):
     c.check(*c.attend())
 
 
-@pytest.fixture(params=["rows", "tile4", "tile8", "tile8x3", "rowsx3"])
+@pytest.fixture(params=["rows", "tile", "tilex3", "rowsx3"])
 def forced(g, request):
     """Every kernel on its own, and sequences split in three whatever their size."""
-    kernel = {"rows": g.GRINQH_ATTEND_ROWS, "tile4": g.GRINQH_ATTEND_TILE_4, "tile8": g.GRINQH_ATTEND_TILE_8}
+    kernel = {"rows": g.GRINQH_ATTEND_ROWS, "tile": g.GRINQH_ATTEND_TILE}
     name, _, splits = request.param.partition("x")
     g.grinqh_set_option(g.GRINQH_OPT_ATTEND_KERNEL, kernel[name])
     g.grinqh_set_option(g.GRINQH_OPT_ATTEND_SPLITS, int(splits or 0))
