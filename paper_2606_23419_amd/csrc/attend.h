@@ -14,8 +14,8 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 
 
 
-// Results of the splits of a sequence: o [split][row * heads + head][D], normalised, and lse (base 2)
-// [split][row * heads + head]; o is not written where lse is -inf.
+// Results of the splits of a block of rows that has more than one (Span::splits): o [split][row * heads + head][D],
+// normalised, and lse (base 2) [split][row * heads + head]; o is not written where lse is -inf.
 struct Partial {
   float* o;
   float* lse;
@@ -26,6 +26,7 @@ struct Partial {
 struct AttendPlan {
   bool tile;        // k_attend_tile, else k_attend_rows
   int nb;           // k_attend_rows: blocks of 16 rows per wave
+  int rows_log2;    // rows of a block: 16 or 32, and 256
   int blocks;       // row blocks of the longest sequence, as far as the caller's estimate goes
   int splits;       // parts of a sequence's tiles, and tiles per part (the last takes the rest)
   int per_split;
@@ -83,6 +84,8 @@ constexpr float kSlack = 6.0f;
 struct Span {
   int sink_tiles, lo_tile, tiles, hi;   // hi: tokens from here on are seen by no row
   __device__ __forceinline__ int tile(int v) const { return v < sink_tiles ? v : v - sink_tiles + lo_tile; }
+  // how many of a call's `most` splits have tiles; a block of one writes its rows itself
+  __device__ __forceinline__ int splits(int most, int per_split) const { return max(1, min(most, (tiles + per_split - 1) / per_split)); }
 };
 
 template <int TK>

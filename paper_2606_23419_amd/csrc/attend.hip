@@ -13,9 +13,9 @@ namespace {
 // one chain of loads.
 constexpr int kJoinThreads = 256;
 
-template <int D, int TYPE>
+template <int D, int TYPE, int TK>
 __global__ __launch_bounds__(kJoinThreads) void k_attend_join(KvCache c, KvBatch b, Attend a, DenseRows out, float* lse,
-                                                              Partial part, int splits, int groups) {
+                                                              Partial part, int most, int per_split, int rows_log2, int groups) {
   constexpr int LPR = D / 8, GROUPS = kJoinThreads / LPR;
   __shared__ float sm[GROUPS], ssum[GROUPS], sy[GROUPS][D];
   const int s = blockIdx.z, lane = threadIdx.x % LPR, group = threadIdx.x / LPR, g = group % groups;
@@ -23,10 +23,14 @@ __global__ __launch_bounds__(kJoinThreads) void k_attend_join(KvCache c, KvBatch
   const long all = (long)sq.n * a.heads;
   const int per_block = GROUPS / groups;
   for (long r0 = (long)blockIdx.x * per_block; r0 < all; r0 += (long)gridDim.x * per_block) {
-    const long r = r0 + group / groups, at = (long)sq.r0 * a.heads + min(r, all - 1);
+    const long r = r0 + group / groups, rc = min(r, all - 1), at = (long)sq.r0 * a.heads + rc;
+    // the row's block, as the kernel before took it, and how many splits that had
+    const int of_group = (int)(rc / a.heads) * a.G + (int)(rc % a.heads) % a.G, first_row = of_group >> rows_log2 << rows_log2;
+    const int last_row = min(first_row + (1 << rows_log2), sq.n * a.G) - 1;
+    const int splits = attend_span<TK>(a, sq.L - sq.n + first_row / a.G, sq.L - sq.n + last_row / a.G).splits(most, per_split);
     float m = -INFINITY, sum = 0, y[8] = {};
     // four splits in flight; past the last one the last is read again and weighs nothing
-    for (int i0 = g; i0 < splits; i0 += 4 * groups) {
+    for (int i0 = splits > 1 ? g : splits; i0 < splits; i0 += 4 * groups) {
       float z[4];
       float4v p[4][2];
 #pragma unroll
@@ -73,7 +77,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_attend_join(KvCache c, KvBatch
       }
       __syncthreads();
     }
-    if (g == 0 && r < all) {
+    if (g == 0 && r < all && splits > 1) {   // else the row is there already
       const float inv = sum == 0 ? 0.0f : 1.0f / sum;
       uint32_t w[4];
       for (int j = 0; j < 4; ++j) w[j] = pack2<TYPE>(y[2 * j] * inv, y[2 * j + 1] * inv);
@@ -90,14 +94,18 @@ AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
   p.tile = forced ? forced != GRINQH_ATTEND_ROWS : R > 32;
   p.nb = R > 16 ? 2 : 1;
   const long per_block = p.tile ? 256 : 16 * p.nb, tile = p.tile ? 64 : 32;
+  p.rows_log2 = __builtin_ctzl(per_block);
   p.blocks = (int)std::min<long>((R + per_block - 1) / per_block, 65535);
   // tiles that the longest sequence's last block sees
   const long seen = a.window ? std::min<long>(a.max_len, (long)a.window + per_block / a.G + a.sinks + 2 * tile) : a.max_len;
   const long tiles = (seen + tile - 1) / tile, groups = (long)B * c.H * p.blocks;
-  const long fill = device_cus();
+  const long fill = p.tile ? device_cus() : 2 * device_cus();
   const long unit = p.tile ? 1 : rows_waves(p.nb), least = p.tile ? 8 : unit;
   long splits = forced_splits ? forced_splits : std::min(std::max<long>(1, fill / groups), std::max<long>(1, tiles / least));
-  if (!forced_splits && !p.tile) splits = std::max(splits, tiles * 32 / 8192);
+  // Sequences enough to fill the CUs without splitting are as a rule of unequal length, which the host does not see:
+  // parts of about 700 tokens keep the longest from being waited for.  32 sequences up to 8191 tokens: 1 part each 99 us,
+  // 3 81, 6 73, 12 65; 16 sequences of 4100 visible tokens 2 57, 4 58, 12 62 (2 and 4 are what filling twice gives there).
+  if (!forced_splits && !p.tile && groups >= device_cus()) splits = std::max(splits, std::min<long>(16, (tiles + 21) / 22));
   long per = (tiles + splits - 1) / splits;
   per = (per + unit - 1) / unit * unit;
   p.per_split = (int)per;
@@ -128,13 +136,19 @@ int launch_attend(const KvCache& c, const KvBatch& b, const Attend& a, const Den
   while (groups < 16 && groups * 2 <= p.splits) groups *= 2;
   const long per_block = kJoinThreads / (c.D / 8) / groups, per_seq = (long)std::min(a.max_rows, b.rows) * a.heads;
   const dim3 grid((unsigned)std::min<long>((per_seq + per_block - 1) / per_block, 1 << 20), 1, b.B);
-  auto go = [&](auto d) {
-    constexpr int D = decltype(d)::value;
-    if (a.type == GRINQH_F16) k_attend_join<D, GRINQH_F16><<<grid, kJoinThreads, 0, s>>>(c, b, a, out, lse, part, p.splits, groups);
-    else k_attend_join<D, GRINQH_BF16><<<grid, kJoinThreads, 0, s>>>(c, b, a, out, lse, part, p.splits, groups);
+  auto go = [&](auto d, auto tk) {
+    constexpr int D = decltype(d)::value, TK = decltype(tk)::value;
+    if (a.type == GRINQH_F16)
+      k_attend_join<D, GRINQH_F16, TK><<<grid, kJoinThreads, 0, s>>>(c, b, a, out, lse, part, p.splits, p.per_split, p.rows_log2, groups);
+    else
+      k_attend_join<D, GRINQH_BF16, TK><<<grid, kJoinThreads, 0, s>>>(c, b, a, out, lse, part, p.splits, p.per_split, p.rows_log2, groups);
   };
-  if (c.D == 64) go(std::integral_constant<int, 64>{});
-  else go(std::integral_constant<int, 128>{});
+  auto on = [&](auto d) {
+    if (p.tile) go(d, std::integral_constant<int, 64>{});
+    else go(d, std::integral_constant<int, 32>{});
+  };
+  if (c.D == 64) on(std::integral_constant<int, 64>{});
+  else on(std::integral_constant<int, 128>{});
   return check_launch("attend");
 }
 

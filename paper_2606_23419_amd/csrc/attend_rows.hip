@@ -94,6 +94,8 @@ void k_attend_rows(AttendArgs args) {
   for (int r0 = blockIdx.y * 16 * NB; r0 < all; r0 += gridDim.y * 16 * NB) {
     const int first = sq.L - sq.n + r0 / a.G, last = sq.L - sq.n + min(r0 + 16 * NB - 1, all - 1) / a.G;
     const Span span = attend_span<kTile>(a, first, last);
+    const int used = span.splits(splits, per_split);
+    if (split >= used) continue;
     const int v_end = split == splits - 1 ? span.tiles : min(span.tiles, (split + 1) * per_split);
     const int v0 = split * per_split + wave;
 
@@ -415,7 +417,7 @@ void k_attend_rows(AttendArgs args) {
         const int rw = sq.r0 + r / a.G, hd = h * a.G + r % a.G;
         const long at = (long)rw * a.heads + hd;
         const float lse2 = rl == 0 ? -INFINITY : rm + log2f(rl);
-        if (splits > 1) {
+        if (used > 1) {
           if (ch == 0) part.lse[split * part.rows + at] = lse2;
           if (lse2 != -INFINITY) {
             float* p = part.o + (split * part.rows + at) * D + ch;

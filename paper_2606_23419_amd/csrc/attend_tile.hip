@@ -85,7 +85,8 @@ void k_attend_tile(AttendArgs args) {
     const int r0 = (blocks - 1 - block) * 32 * kWaves;
     const int first = sq.L - sq.n + r0 / a.G, last = sq.L - sq.n + min(r0 + 32 * kWaves - 1, all - 1) / a.G;
     const Span span = attend_span<kTile>(a, first, last);
-    const int v0 = split * per_split;
+    const int v0 = split * per_split, used = span.splits(splits, per_split);
+    if (split >= used) continue;
     const int v_end = split == splits - 1 ? span.tiles : min(span.tiles, v0 + per_split);
 
     // this lane's row (both halves of the wave have the same 32), and the span of the wave's rows
@@ -526,7 +527,7 @@ void k_attend_tile(AttendArgs args) {
     const float lse2 = l == 0 ? -INFINITY : m + log2f(l);
     if (w0 + (lane & 31) < all) {
       const long at = (long)row * a.heads + head;
-      if (splits > 1) {
+      if (used > 1) {
         if (half == 0) part.lse[split * part.rows + at] = lse2;
         if (lse2 != -INFINITY) {
           float* p = part.o + (split * part.rows + at) * D + 4 * half;

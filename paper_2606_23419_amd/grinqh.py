@@ -105,7 +105,7 @@ class _Rows(ctypes.Structure):
 
 
 # The arrays of a cache and of a batch, as grinqh.h lays them out.  They keep the C structure made of them, which is
-# used again as long as it was checked against the same descriptor and every array is where it was.
+# used again as long as it was checked against the same descriptor and every array is where and as it was.
 class KvCache(collections.namedtuple("KvCache", "k v k_scale v_scale")):
     pass
 
@@ -525,12 +525,16 @@ def _kv_type(format):
     return {GRINQH_KV_F16: torch.float16, GRINQH_KV_BF16: torch.bfloat16, GRINQH_KV_I8: torch.int8}[format]
 
 
+_ROW_TYPES = {}
+
+
 def _row_type(dtype, name):
-    torch = _torch()
-    types = {torch.float16: GRINQH_F16, torch.bfloat16: GRINQH_BF16, torch.float32: GRINQH_F32}
-    if dtype not in types:
+    if not _ROW_TYPES:
+        torch = _torch()
+        _ROW_TYPES.update({torch.float16: GRINQH_F16, torch.bfloat16: GRINQH_BF16, torch.float32: GRINQH_F32})
+    if dtype not in _ROW_TYPES:
         raise TypeError(f"{name} must be fp16, bf16 or fp32, got {dtype}")
-    return types[dtype]
+    return _ROW_TYPES[dtype]
 
 
 def kv_cache(desc: KvDesc, device="cuda") -> KvCache:
@@ -545,7 +549,7 @@ def kv_cache(desc: KvDesc, device="cuda") -> KvCache:
 
 
 def _cache_args(desc, cache):
-    at = [t.data_ptr() if t is not None else None for t in cache]
+    at = [(t.data_ptr(), t.shape, t.stride()) if t is not None else None for t in cache]
     key = (desc.format, desc.heads, desc.head_dim, desc.page, desc.n_pages, at)
     kept = cache.__dict__.get("_args")
     if kept is not None and kept[0] == key:
@@ -565,7 +569,7 @@ def _cache_args(desc, cache):
 
 
 def _batch_args(batch, rows):
-    key = (int(rows), batch.block_table.data_ptr(), batch.seq_lens.data_ptr(), batch.row_offsets.data_ptr())
+    key = (int(rows), [(t.data_ptr(), t.shape, t.stride()) for t in batch])
     kept = batch.__dict__.get("_args")
     if kept is not None and kept[0] == key:
         return kept[1]
@@ -589,7 +593,7 @@ def _rows(t, dtype, name, shape):
         raise ValueError(f"{name} must be a device tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     r, h, d = t.stride()
     if d != 1:
@@ -670,9 +674,9 @@ def grinqh_attend(desc: KvDesc, cache: KvCache, batch: KvBatch, q, scale=None, w
     a = _attend_desc(desc, heads, _row_type(q.dtype, "q"), scale, window, sinks,
                      max(1, rows) if max_rows is None else max_rows,
                      max(1, min(b.table_width * desc.page, 1 << 30)) if max_len is None else max_len)
-    n = ctypes.c_size_t()
-    _check(lib.grinqh_attend_workspace_bytes(ctypes.byref(desc), ctypes.byref(a), b.B, rows, ctypes.byref(n)))
     if workspace is None:
+        n = ctypes.c_size_t()
+        _check(lib.grinqh_attend_workspace_bytes(ctypes.byref(desc), ctypes.byref(a), b.B, rows, ctypes.byref(n)))
         workspace = torch.empty(n.value, dtype=torch.uint8, device=q.device)
         _held_for(stream, workspace)
     wp = _dev(workspace, torch.uint8, "workspace") if workspace.numel() else None
