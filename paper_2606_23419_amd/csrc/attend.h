@@ -58,7 +58,9 @@ __device__ __forceinline__ const AttendArgs& late() {
 }
 
 // Waves per workgroup of k_attend_rows, and per SIMD: of one block of 16 rows three (8-bit) or two workgroups of
-// four waves share a CU, so that one's start and end overlap with the others' loads.
+// four waves share a CU, so that one's start and end overlap with the others' loads.  One token over 131072 tokens,
+// 8 bits, whole call: 60 us, with workgroups of 8, 12 and 16 waves 59 .. 93; 32 sequences up to 8191 tokens 67 .. 75
+// and 75 .. 130 (over the numbers of parts).
 constexpr int rows_waves(int nb) { return nb == 1 ? 4 : 8; }
 constexpr int rows_per_simd(int format, int nb) { return format == GRINQH_KV_I8 && nb == 1 ? 3 : 2; }
 
@@ -128,12 +130,6 @@ template <int FORMAT>
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   constexpr uint32_t e = FORMAT == GRINQH_KV_F16 ? 0x7c00u : 0x7f80u;
   return ((w & e) == e ? 0xffffu : 0u) | ((w >> 16 & e) == e ? 0xffff0000u : 0u);
-}
-
-// The larger of each half, as unsigned numbers.
-__device__ __forceinline__ uint32_t max_halves(uint32_t x, uint32_t y) {
-  typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, x), __builtin_bit_cast(ushort2v, y)));
 }
 
 

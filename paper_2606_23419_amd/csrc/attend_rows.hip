@@ -12,6 +12,11 @@
 //   - pages of 16 tokens or more hold a block whole: its address is scalar, the lanes' offsets are constant.
 //     Smaller pages (SMALL) pass the 32 tokens' addresses and scales through LDS.
 // The next tile's K is loaded while the softmax runs, its V behind the second product.
+//
+// Bound by memory: every visible K and V row is read once.  One token over 131072 tokens of an 8-bit cache, 8 kv heads
+// of 128 (277 MB): 44.6 us in this kernel, 6.2 TB/s where a plain read of 2 GiB reaches 6.9, and 4.8 us joining 64
+// parts; 32 sequences up to 8191 tokens, bf16 rows (269 MB): 51 and 5 us.  A part of a few tiles is a chain of latencies
+// (page id, loads, two products): one token after 76 takes 6.1 us, of which its 0.2 MB are nothing.
 #include "attend.h"
 
 namespace grinqh {

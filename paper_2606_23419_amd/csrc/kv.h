@@ -87,4 +87,10 @@ size_t attend_workspace(const KvCache& c, const Attend& a, int B, int rows);
 int launch_attend(const KvCache& c, const KvBatch& b, const Attend& a, const DenseRows& q, const DenseRows& out,
                   float* lse, void* workspace, hipStream_t s);
 
+// The larger of each half, as unsigned numbers.
+__device__ __forceinline__ uint32_t max_halves(uint32_t x, uint32_t y) {
+  typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, x), __builtin_bit_cast(ushort2v, y)));
+}
+
 }  // namespace grinqh
