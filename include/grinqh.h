@@ -380,7 +380,8 @@ typedef struct {
  * row NaN, pages that no row sees may have any id.
  * Precision: scores, statistics and sums in fp32; exp(s_t - m), at an 8-bit
  * cache times the value's scale, is rounded to 16 bits for the product with
- * the values (fp16, for a bf16 cache bf16).
+ * the values (fp16, for a bf16 cache bf16); at an 8-bit cache 11 bits of it
+ * stay down to value scales 2^23 below the largest that the row has seen.
  * The rows' own tokens have to be in the cache already (grinqh_kv_write).
  * workspace: device, 16-byte aligned, of at least the size that
  * grinqh_attend_workspace_bytes gives for the same arguments (host only; may

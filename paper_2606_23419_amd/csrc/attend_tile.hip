@@ -13,10 +13,11 @@
 // broadcasts by DPP.  Tiles are copied several slots ahead, and the waves run in two halves half a tile apart: one
 // half's products meet the other's softmax.
 //
-// Bound by the matrix cores and what feeds them: 4 D operations per row and visible token.  4096 rows of 32 heads
-// behind 32768 tokens of an 8-bit cache (2.34 Tflop): 2.68 ms, 870 TFLOP/s, where a library product of 8192^3 reaches
-// 1200.  What is left is the staging (page addresses, issue of the copies, a workgroup's first tile) and the weights'
-// exponentials beside the products; copies spread among the products were faster at D = 64 (541 -> 472 us) and slower
+// Bound by the vector unit beside the matrix cores: 4 D operations per row and visible token in products of 32 cycles, and
+// with each at 8 bits about nine other vector instructions (scales, maximum, exponential, sum, packing, codes to fp16).
+// 4096 rows of 32 heads behind 32768 tokens of an 8-bit cache (2.34 Tflop): 2.68 ms, 870 TFLOP/s, where a library product
+// of 8192^3 reaches 1200; the products hold their pipe 0.36 of the time.  16-bit caches pay for the staging (page addresses,
+// issue of the copies, a workgroup's first tile): without it in the loop they came to 1300; copies spread among the products were faster at D = 64 (541 -> 472 us) and slower
 // at D = 128, so they stand together.  A workgroup takes about 10 us to start and end and 2.1 us per tile: a prompt of 2048
 // tokens from its start (34 Gflop, 8 kv heads of 4) is 256 workgroups of 4 to 32 tiles, and the longest makes its 72 us.
 #include "attend.h"
