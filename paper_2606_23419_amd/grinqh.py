@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import functools
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -224,6 +225,7 @@ def grinqh_workspace_bytes(desc: LayerDesc, B: int) -> int:
 
 
 # ----------------------------------------------------------- device calls --
+@functools.lru_cache(maxsize=None)
 def _torch():
     import torch
     return torch
@@ -245,9 +247,11 @@ def _dev(t, dtype, name, shape=None):
 
 
 def _stream(stream):
-    torch = _torch()
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    # torch.cuda.current_stream().cuda_stream without the stream object: 0.3 us of a call in place of 3
+    c = _torch()._C
+    return ctypes.c_void_p(c._cuda_getCurrentRawStream(c._cuda_getDevice()))
 
 
 def grinqh_pack(desc: LayerDesc, W=None, codes=None, scales=None, out_codes=None,
