@@ -325,11 +325,12 @@ typedef struct {
   const int32_t* row_offsets;  /* device [B + 1]: where each sequence's rows start */
   int32_t B;                   /* sequences, 0..65535 */
   int32_t table_width;         /* page ids per sequence, >= 1 */
-  int32_t rows;                /* rows of the dense arrays, 0..2^24 */
+  int32_t rows;                /* rows of the dense arrays, 0..2^24; in attention times the
+                                  query heads at most 2^30 */
 } grinqh_kv_batch;
 
 /* Dense rows [rows][heads][head_dim]: the last axis contiguous, the others with
- * strides in elements, >= 0 and multiples of 16 bytes; base 16-byte aligned.
+ * strides in elements, 0..2^36 and multiples of 16 bytes; base 16-byte aligned.
  * Rows that are written must not overlap. */
 typedef struct {
   void* data;

@@ -57,8 +57,8 @@ static int check_rows(const char* name, const grinqh_rows* in, int size, int row
   if (!in || !in->data) return fail(GRINQH_EINVAL, "%s must not be NULL", name);
   if ((uintptr_t)in->data & 15u) return fail(GRINQH_EINVAL, "%s must be 16-byte aligned", name);
   // the stride of an axis of one entry says nothing
-  const int64_t rs = rows > 1 ? in->row_stride : 0, hs = heads > 1 ? in->head_stride : 0, most = (int64_t)1 << 40;
-  if (rs < 0 || hs < 0 || rs > most || hs > most) return fail(GRINQH_EINVAL, "%s: strides outside 0..2^40", name);
+  const int64_t rs = rows > 1 ? in->row_stride : 0, hs = heads > 1 ? in->head_stride : 0, most = (int64_t)1 << 36;
+  if (rs < 0 || hs < 0 || rs > most || hs > most) return fail(GRINQH_EINVAL, "%s: strides outside 0..2^36", name);
   if ((rs * size) % 16 || (hs * size) % 16) return fail(GRINQH_EINVAL, "%s: strides must be multiples of 16 bytes", name);
   // rows of heads, or heads of rows, one after the other
   const bool apart = (hs >= dim || heads == 1) && (rs >= (heads - 1) * hs + dim || rows == 1);
@@ -142,6 +142,13 @@ int grinqh_kv_read(const grinqh_kv_desc* desc, const grinqh_kv_cache* cache, con
   return launch_kv_read(c, b, type, kr, vr, (hipStream_t)stream);
 }
 
+// Rows times heads, and the rows of a kv head rounded up to a workgroup's, fit 32 bits.
+static int check_attend_rows(const Attend& a, int rows) {
+  if ((int64_t)rows * a.heads > (1 << 30))
+    return fail(GRINQH_ESIZE, "rows=%d of %d heads are more than 2^30", rows, a.heads);
+  return GRINQH_OK;
+}
+
 int grinqh_attend_workspace_bytes(const grinqh_kv_desc* desc, const grinqh_attend_desc* attend, int32_t B, int32_t rows,
                                   size_t* bytes) {
   clear_error();
@@ -151,6 +158,7 @@ int grinqh_attend_workspace_bytes(const grinqh_kv_desc* desc, const grinqh_atten
   if (st || (st = resolve_attend(c, attend, &a))) return st;
   if (B < 0 || B > 65535) return fail(GRINQH_EINVAL, "B=%d outside 0..65535", B);
   if (rows < 0 || rows > (1 << 24)) return fail(GRINQH_EINVAL, "rows=%d outside 0..2^24", rows);
+  if ((st = check_attend_rows(a, rows))) return st;
   if (!bytes) return fail(GRINQH_EINVAL, "bytes is NULL");
   *bytes = B && rows ? attend_workspace(c, a, B, rows) : 0;
   return GRINQH_OK;
@@ -167,6 +175,7 @@ int grinqh_attend(const grinqh_kv_desc* desc, const grinqh_kv_cache* cache, cons
   int st = resolve_kv(desc, &c);
   if (st || (st = resolve_attend(c, attend, &a)) || (st = check_cache(cache, &c)) || (st = check_batch(batch, &b))) return st;
   if (!b.B || !b.rows) return GRINQH_OK;
+  if ((st = check_attend_rows(a, b.rows))) return st;
   if ((st = check_rows("q", q, 2, b.rows, a.heads, c.D, false, &qr))) return st;
   if ((st = check_rows("out", out, 2, b.rows, a.heads, c.D, true, &outr))) return st;
   if ((uintptr_t)lse & 3u) return fail(GRINQH_EINVAL, "lse must be 4-byte aligned");

@@ -119,3 +119,17 @@ def test_workspace_size_is_a_host_matter(g):
     for B, rows, status in [(2, 6, 0), (0, 0, 0), (-1, 6, -1), (2, -1, -1)]:
         assert g.lib.grinqh_attend_workspace_bytes(ctypes.byref(desc(g)), ctypes.byref(adesc(g)), B, rows, ctypes.byref(n)) == status
     assert g.lib.grinqh_attend_workspace_bytes(ctypes.byref(desc(g)), ctypes.byref(adesc(g)), 2, 6, None) == g.GRINQH_EINVAL
+
+
+def test_rows_times_heads_fit_32_bits(g):
+    n, rows = ctypes.c_size_t(), 1 << 24
+    for heads, status in ((64, g.GRINQH_OK), (72, g.GRINQH_ESIZE)):
+        a = adesc(g, heads=heads)
+        assert g.lib.grinqh_attend_workspace_bytes(ctypes.byref(desc(g)), ctypes.byref(a), 2, rows, ctypes.byref(n)) == status
+    assert attend(g, desc(g), a, batch=(P, P, P, 2, 4, rows)) == g.GRINQH_ESIZE
+
+
+@pytest.mark.parametrize("q", [(P, (1 << 36) + 8, 128), (P, 4096, (1 << 36) + 8)])
+def test_strides_are_bounded(g, q):
+    assert attend(g, desc(g), adesc(g), q=q) == g.GRINQH_EINVAL
+    assert attend(g, desc(g), adesc(g), out=q) == g.GRINQH_EINVAL
