@@ -39,6 +39,13 @@ __device__ __forceinline__ T load_global(const void* p) {
   return *(const __attribute__((address_space(1))) T*)p;
 }
 
+// Between a wave's writes to LDS and its reads of them.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // The attention kernels' argument.  What only the start or the end of a kernel needs is read there (late()):
 // held in scalar registers throughout, it would push other values out of them.
 struct AttendArgs {

@@ -40,12 +40,6 @@ __device__ __forceinline__ uint32_t infinite_ones(uint32_t w, int sign) {
   return r;
 }
 
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // LDS of one wave: where the tile's 32 tokens lie, and their scales.
 struct alignas(16) WaveTokens {
   const char* k[kTile];

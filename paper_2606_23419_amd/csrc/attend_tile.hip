@@ -18,8 +18,8 @@
 // 4096 rows of 32 heads behind 32768 tokens of an 8-bit cache (2.34 Tflop): 2.68 ms, 870 TFLOP/s, where a library product
 // of 8192^3 reaches 1200; the products hold their pipe 0.36 of the time.  16-bit caches pay for the staging (page addresses,
 // issue of the copies, a workgroup's first tile): without it in the loop they came to 1300; copies spread among the products were faster at D = 64 (541 -> 472 us) and slower
-// at D = 128, so they stand together.  A workgroup takes about 10 us to start and end and 2.1 us per tile: a prompt of 2048
-// tokens from its start (34 Gflop, 8 kv heads of 4) is 256 workgroups of 4 to 32 tiles, and the longest makes its 72 us.
+// at D = 128, so they stand together.  A call of one tile takes 12 us, and 1.8 to 2.2 us go with every further one: a prompt
+// of 2048 tokens from its start (34 Gflop, 8 kv heads of 4) is 256 workgroups of 4 to 32 tiles, and the longest makes its 75 us.
 #include "attend.h"
 
 namespace grinqh {
@@ -525,6 +525,7 @@ void k_attend_tile(AttendArgs args) {
       }
       if (!second) end_slot();
       wait(true);
+      __syncthreads();
     }
 
     const DenseRows out = late().out;
@@ -548,13 +549,29 @@ void k_attend_tile(AttendArgs args) {
         }
       } else {
         if (lse && half == 0) lse[at] = lse2 * kLn2;
-        char* p = out.p + (row * out.row + head * out.head + 4 * half) * 2;
+      }
+    }
+    if (used == 1) {
+      // Rows of the output are written whole, through LDS: from the lanes' own pieces of 8 bytes every store would touch 32
+      // rows, 2 us of a workgroup's end.  (`rows` begins where no copy is under way any more.)
+      constexpr int STRIDE = RB + 16;        // 16 rows of pieces meet 64 banks
+      static_assert(kWaves * 32 * STRIDE <= sizeof(lds.k) + sizeof(lds.v));
+      uint8_t* rows = &lds.k[0][0][0] + wave * 32 * STRIDE;
 #pragma unroll
-        for (int j = 0; j < VB; ++j)
+      for (int j = 0; j < VB; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            *(u32x2*)(p + 2 * (32 * j + 8 * e)) = u32x2{pack2<TYPE>(o[j][4 * e] * inv, o[j][4 * e + 1] * inv),
-                                                        pack2<TYPE>(o[j][4 * e + 2] * inv, o[j][4 * e + 3] * inv)};
+        for (int e = 0; e < 4; ++e)
+          *(u32x2*)(rows + (lane & 31) * STRIDE + 2 * (32 * j + 8 * e + 4 * half)) =
+              u32x2{pack2<TYPE>(o[j][4 * e] * inv, o[j][4 * e + 1] * inv), pack2<TYPE>(o[j][4 * e + 2] * inv, o[j][4 * e + 3] * inv)};
+      const long to = (row * out.row + head * out.head) * 2;
+      wave_sync();
+      constexpr int LANES = RB / 16;         // of a row
+#pragma unroll
+      for (int x = 0; x < LANES / 2; ++x) {
+        const int n = x * (64 / LANES) + lane / LANES, piece = 16 * (lane % LANES);
+        const u32x4 w = *(const u32x4*)(rows + n * STRIDE + piece);
+        const long at = __shfl(to, n);
+        if (w0 + n < all) *(u32x4*)(out.p + at + piece) = w;
       }
     }
     __syncthreads();
