@@ -91,10 +91,11 @@ AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
   AttendPlan p = {};
   const int forced = option(&Options::attend_kernel), forced_splits = option(&Options::attend_splits);
   const long n = std::min(a.max_rows, rows), R = n * a.G;
-  // R rows of a kv head share its K and V.  Up to 32 of them are one workgroup's in k_attend_rows, more would read the
-  // cache again.  4 sequences of 8190 tokens, 8 bits, 4 heads a group: R = 32 rows kernel 38 us, tile kernel 42 .. 48 (over
-  // the numbers of parts); R = 64 rows kernel 54, tile kernel 48 .. 53.
-  p.tile = forced ? forced != GRINQH_ATTEND_ROWS : R > 32;
+  // R rows of a kv head share its K and V.  Up to 32 of them are one workgroup's in k_attend_rows, the next read the cache
+  // again, from L2 at first.  8 bits, rows kernel against tile kernel, us: R = 64 over 8190 tokens of 1 sequence 26 : 36, of
+  // 4 42 : 58; 500 tokens of 4 17 : 33; 2000 of 32 97 : 98; 16 bits, 8190 of 8 91 : 102.  R = 128: 34 : 39, 60 : 66,
+  // 19 : 34, 182 : 101, 214 : 110.
+  p.tile = forced ? forced != GRINQH_ATTEND_ROWS : R > 64;
   p.nb = R > 16 ? 2 : 1;
   const long per_block = p.tile ? 256 : 16 * p.nb, tile = p.tile ? 64 : 32;
   p.rows_log2 = __builtin_ctzl(per_block);
@@ -104,7 +105,7 @@ AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
   const long tiles = (seen + tile - 1) / tile, groups = (long)B * c.H * p.blocks;
   // Sequences too few to fill the device are split: one workgroup per CU in k_attend_tile (its LDS), two and more in
   // k_attend_rows.  One token over 131072 tokens is 64 parts: 16 parts 71 us, 32 62, 64 58, 128 64.  Prompts that fill half
-  // the CUs stay whole: 2048 rows of 32 heads from the start 78 us, in two parts 91 and 23 joining.
+  // the CUs stay whole: 2048 rows of 32 heads from the start 74 us, in two parts 85 and 23 joining, in three 71 and 25.
   const long fill = p.tile ? device_cus() : 2 * device_cus();
   const long unit = p.tile ? 1 : rows_waves(p.nb), least = p.tile ? 8 : unit;
   long splits = forced_splits ? forced_splits : std::min(std::max<long>(1, fill / groups), std::max<long>(1, tiles / least));

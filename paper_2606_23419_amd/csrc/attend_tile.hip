@@ -15,11 +15,11 @@
 //
 // Bound by the vector unit beside the matrix cores: 4 D operations per row and visible token in products of 32 cycles, and
 // with each at 8 bits about nine other vector instructions (scales, maximum, exponential, sum, packing, codes to fp16).
-// 4096 rows of 32 heads behind 32768 tokens of an 8-bit cache (2.34 Tflop): 2.68 ms, 870 TFLOP/s, where a library product
-// of 8192^3 reaches 1200; the products hold their pipe 0.36 of the time.  16-bit caches pay for the staging (page addresses,
+// 4096 rows of 32 heads behind 32768 tokens of an 8-bit cache (2.34 Tflop): 2.68 .. 2.83 ms, 825 .. 870 TFLOP/s, where a library
+// product of 8192^3 reaches 1200; the products hold their pipe 0.36 of the time.  16-bit caches pay for the staging (page addresses,
 // issue of the copies, a workgroup's first tile): without it in the loop they came to 1300; copies spread among the products were faster at D = 64 (541 -> 472 us) and slower
 // at D = 128, so they stand together.  A call of one tile takes 12 us, and 1.8 to 2.2 us go with every further one: a prompt
-// of 2048 tokens from its start (34 Gflop, 8 kv heads of 4) is 256 workgroups of 4 to 32 tiles, and the longest makes its 75 us.
+// of 2048 tokens from its start (34 Gflop, 8 kv heads of 4) is 256 workgroups of 4 to 32 tiles, and the longest makes its 74 us.
 #include "attend.h"
 
 namespace grinqh {
