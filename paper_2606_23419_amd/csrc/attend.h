@@ -88,6 +88,19 @@ constexpr float kLn2 = 0.6931471805599453f;
 // stay under 2^6 and the sums are rescaled a few times instead of at every tile.
 constexpr float kSlack = 6.0f;
 
+// A score times its factor, rounded to fp32 whatever is done with it next.
+__device__ __forceinline__ float rounded_product(float x, float factor) {
+#pragma clang fp contract(off)
+  return x * factor;
+}
+// From 2^23 on the spacing of fp32 is one power of two and more.  exp2(fma(score, factor, -m)) would see the rest by which the
+// largest product was rounded to m, and make that token's weight anything from nothing to infinity: the products of a row
+// that is held against such an m are rounded first, as m was.  Its slack is -inf, so every tile takes the branch that does so.
+__device__ __forceinline__ bool far_out(float m) { return fabsf(m) >= 0x1p23f && fabsf(m) < INFINITY; }
+// 1 / factor for factors of 2^-124 and more (those of such rows are 2^-105 and more), to rcp's last bit; the instruction
+// itself makes zero of a quotient under 2^-126.
+__device__ __forceinline__ float inverse(float factor) { return __builtin_amdgcn_rcpf(0.25f * factor) * 0.25f; }
+
 // The tiles of TK tokens that some of the rows at positions first .. last see: those of the sinks, then
 // from the window's start on.
 struct Span {

@@ -134,12 +134,12 @@ void k_attend_rows(AttendArgs args) {
       }
     }
 
-    float m[NB], l[NB];
+    float m[NB], l[NB], slack[NB];
     float4v o[NB][VC];
     int ev[NB];                              // of the values' scales that the row has seen (8-bit cache)
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      m[n] = -INFINITY; l[n] = 0; ev[n] = kLowestExponent;
+      m[n] = -INFINITY; l[n] = 0; ev[n] = kLowestExponent; slack[n] = kSlack;
 #pragma unroll
       for (int j = 0; j < VC; ++j) o[n][j] = float4v{0, 0, 0, 0};
     }
@@ -286,20 +286,31 @@ void k_attend_rows(AttendArgs args) {
         float mx = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e) mx = fmaxf(mx, sc[n][e >> 2][e & 3]);
-        mx = max_xor16(max_xor32(mx)) * factor[n];
+        mx = rounded_product(max_xor16(max_xor32(mx)), factor[n]);
         const int big = I8 ? scale_exponent(max_xor16(max_xor32(vmax))) : kLowestExponent;
         // what a row is held against follows its own scores and values alone: other rows, and what
         // they see, never change its bits
-        const bool rises = mx > m[n] + kSlack, grows = I8 && big > ev[n];
-        if (__any(rises || grows)) {
+        const bool grows = I8 && big > ev[n];
+        float held = m[n];
+        if (__any(mx > m[n] + slack[n] || grows)) {
+          const bool rises = mx - m[n] > kSlack;
           float alpha = rises ? exp2f(m[n] - mx) : 1.0f;
           if (rises) m[n] = mx;
           l[n] *= alpha;
           if (grows) { alpha *= ldexpf(1.0f, max(ev[n] - big, -126)); ev[n] = big; }
 #pragma unroll
           for (int j = 0; j < VC; ++j) o[n][j] *= alpha;
+          held = m[n];
+          slack[n] = far_out(held) ? -INFINITY : kSlack;
+          if (far_out(held)) {   // what exp2 is to see, over the factor that it will be multiplied by
+            const float inv = inverse(factor[n]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sc[n][e >> 2][e & 3] = (rounded_product(sc[n][e >> 2][e & 3], factor[n]) - held) * inv;
+            held = 0;
+          }
         }
-        const float base = m[n] == -INFINITY ? 0.0f : m[n], down = I8 ? ldexpf(1.0f, kUp - ev[n]) : 1.0f;
+        const float down = I8 ? ldexpf(1.0f, kUp - ev[n]) : 1.0f;
+        const float base = held == -INFINITY ? 0.0f : held;
         float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {

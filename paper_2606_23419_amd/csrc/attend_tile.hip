@@ -134,7 +134,7 @@ void k_attend_tile(AttendArgs args) {
       }
     }
 
-    float m = -INFINITY, l = 0;
+    float m = -INFINITY, l = 0, slack = kSlack;
     int ev = kLowestExponent;
     float16v o[VB];
 #pragma unroll
@@ -401,11 +401,13 @@ void k_attend_tile(AttendArgs args) {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[t][e]);
-      mx = max_xor32(mx) * factor;
+      mx = rounded_product(max_xor32(mx), factor);
       look(i + 4);   // here: a scalar load among reads of LDS would make every wait for them a wait for all
       // a row's own scores and values alone decide what it is held against
-      const bool rises = mx > m + kSlack, grows = I8 && big > ev;
-      if (__any(rises || grows)) {
+      const bool grows = I8 && big > ev;
+      float held = m;
+      if (__any(mx - m > slack || grows)) {
+        const bool rises = mx - m > kSlack;
         float alpha = rises ? exp2f(m - mx) : 1.0f;
         if (rises) m = mx;
         l *= alpha;
@@ -414,8 +416,18 @@ void k_attend_tile(AttendArgs args) {
         for (int j = 0; j < VB; ++j)
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[j][e] *= alpha;
+        held = m;
+        slack = far_out(held) ? -INFINITY : kSlack;
+        if (far_out(held)) {   // what exp2 is to see, over the factor that it will be multiplied by
+          const float inv = inverse(factor);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[t][e] = (rounded_product(sc[t][e], factor) - held) * inv;
+          held = 0;
+        }
       }
-      const float base = m == -INFINITY ? 0.0f : m;
+      const float base = held == -INFINITY ? 0.0f : held;
       // the factor 2^(kUp - ev) goes into the tokens' scales, which the wave shares: that of the largest ev,
       // and where rows differ what is left of theirs (powers of two: exact)
       float down = 1, fix = 1;
