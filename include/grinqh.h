@@ -381,8 +381,10 @@ typedef struct {
  * row NaN, pages that no row sees may have any id.
  * Precision: scores, statistics and sums in fp32; exp(s_t - m), at an 8-bit
  * cache times the value's scale, is rounded to 16 bits for the product with
- * the values (fp16, for a bf16 cache bf16); at an 8-bit cache 11 bits of it
- * stay down to value scales 2^23 below the largest that the row has seen.
+ * the values (fp16, for a bf16 cache bf16).  In fp16 11 bits of it stay down
+ * to 2^-23 of the row's largest weight, at an 8-bit cache to value scales 2^23
+ * below the largest that the row has seen; what is below is off by at most
+ * 2^-34 (2^-33 at 8 bits) of the largest.
  * The rows' own tokens have to be in the cache already (grinqh_kv_write).
  * workspace: device, 16-byte aligned, of at least the size that
  * grinqh_attend_workspace_bytes gives for the same arguments (host only; may

@@ -84,19 +84,28 @@ static __device__ const uint32_t g_nans[kFill] = {NAN64, NAN64, NAN64, NAN64, NA
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-// The running maximum follows the scores once they pass it by this many powers of two, so weights
-// stay under 2^6 and the sums are rescaled a few times instead of at every tile.
-constexpr float kSlack = 6.0f;
+// What a row's scores are held against follows their maximum once that has risen by kSlack powers of two, so weights stay under
+// 2^6 of the maximum's and the sums are rescaled a few times instead of at every tile.  For an fp16 cache it stands kLift
+// powers of two below the maximum: weights are at most 2^15 then, 11 bits of them stay down to 2^-23 of a row's largest, and what
+// is below is off by at most 2^-34 of it.  (Held against the maximum itself, a long tail 17 nats below a first token would be
+// rounded to nothing and stay in the sum that divides.)
+template <int FORMAT>
+constexpr float kLift = FORMAT == GRINQH_KV_F16 ? 9.0f : 0.0f;
+template <int FORMAT>
+constexpr float kSlack = 6.0f + kLift<FORMAT>;
 
 // A score times its factor, rounded to fp32 whatever is done with it next.
 __device__ __forceinline__ float rounded_product(float x, float factor) {
 #pragma clang fp contract(off)
   return x * factor;
 }
-// From 2^23 on the spacing of fp32 is one power of two and more.  exp2(fma(score, factor, -m)) would see the rest by which the
+// From 2^22 on the spacing of fp32 is half a power of two and more.  exp2(fma(score, factor, -m)) would see the rest by which the
 // largest product was rounded to m, and make that token's weight anything from nothing to infinity: the products of a row
-// that is held against such an m are rounded first, as m was.  Its slack is -inf, so every tile takes the branch that does so.
-__device__ __forceinline__ bool far_out(float m) { return fabsf(m) >= 0x1p23f && fabsf(m) < INFINITY; }
+// that is held against such an m, which is not lifted, are rounded first, as m was.  Its slack is -inf, so every tile takes the
+// branch that does so.
+__device__ __forceinline__ bool far_out(float m) { return fabsf(m) >= 0x1p22f && fabsf(m) < INFINITY; }
+template <int FORMAT>
+__device__ __forceinline__ float held_against(float mx) { return far_out(mx) ? mx : mx - kLift<FORMAT>; }
 // 1 / factor for factors of 2^-124 and more (those of such rows are 2^-105 and more), to rcp's last bit; the instruction
 // itself makes zero of a quotient under 2^-126.
 __device__ __forceinline__ float inverse(float factor) { return __builtin_amdgcn_rcpf(0.25f * factor) * 0.25f; }

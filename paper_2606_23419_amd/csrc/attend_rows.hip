@@ -139,7 +139,7 @@ void k_attend_rows(AttendArgs args) {
     int ev[NB];                              // of the values' scales that the row has seen (8-bit cache)
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      m[n] = -INFINITY; l[n] = 0; ev[n] = kLowestExponent; slack[n] = kSlack;
+      m[n] = -INFINITY; l[n] = 0; ev[n] = kLowestExponent; slack[n] = kSlack<FORMAT>;
 #pragma unroll
       for (int j = 0; j < VC; ++j) o[n][j] = float4v{0, 0, 0, 0};
     }
@@ -293,15 +293,16 @@ void k_attend_rows(AttendArgs args) {
         const bool grows = I8 && big > ev[n];
         float held = m[n];
         if (__any(mx > m[n] + slack[n] || grows)) {
-          const bool rises = mx - m[n] > kSlack;
-          float alpha = rises ? exp2f(m[n] - mx) : 1.0f;
-          if (rises) m[n] = mx;
+          const bool rises = mx - m[n] > kSlack<FORMAT>;
+          const float was = m[n];
+          if (rises) m[n] = held_against<FORMAT>(mx);
+          float alpha = rises ? exp2f(was - m[n]) : 1.0f;
           l[n] *= alpha;
           if (grows) { alpha *= ldexpf(1.0f, max(ev[n] - big, -126)); ev[n] = big; }
 #pragma unroll
           for (int j = 0; j < VC; ++j) o[n][j] *= alpha;
           held = m[n];
-          slack[n] = far_out(held) ? -INFINITY : kSlack;
+          slack[n] = far_out(held) ? -INFINITY : kSlack<FORMAT>;
           if (far_out(held)) {   // what exp2 is to see, over the factor that it will be multiplied by
             const float inv = inverse(factor[n]);
 #pragma unroll

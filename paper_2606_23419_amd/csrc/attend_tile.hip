@@ -134,7 +134,7 @@ void k_attend_tile(AttendArgs args) {
       }
     }
 
-    float m = -INFINITY, l = 0, slack = kSlack;
+    float m = -INFINITY, l = 0, slack = kSlack<FORMAT>;
     int ev = kLowestExponent;
     float16v o[VB];
 #pragma unroll
@@ -407,9 +407,10 @@ void k_attend_tile(AttendArgs args) {
       const bool grows = I8 && big > ev;
       float held = m;
       if (__any(mx - m > slack || grows)) {
-        const bool rises = mx - m > kSlack;
-        float alpha = rises ? exp2f(m - mx) : 1.0f;
-        if (rises) m = mx;
+        const bool rises = mx - m > kSlack<FORMAT>;
+        const float was = m;
+        if (rises) m = held_against<FORMAT>(mx);
+        float alpha = rises ? exp2f(was - m) : 1.0f;
         l *= alpha;
         if (grows) { alpha *= ldexpf(1.0f, max(ev - big, -126)); ev = big; }
 #pragma unroll
@@ -417,7 +418,7 @@ void k_attend_tile(AttendArgs args) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[j][e] *= alpha;
         held = m;
-        slack = far_out(held) ? -INFINITY : kSlack;
+        slack = far_out(held) ? -INFINITY : kSlack<FORMAT>;
         if (far_out(held)) {   // what exp2 is to see, over the factor that it will be multiplied by
           const float inv = inverse(factor);
 #pragma unroll

@@ -54,3 +54,64 @@ def test_scores_past_the_integers_of_fp32(g, torch, forced, fmt, type, n, L):  #
     bound = 0 if fmt != "i8" else (U[type] + 2.0 ** -11 + 2.0 ** -20) * np.abs(ref)
     assert (np.abs(down(out) - ref) <= bound).all()
     assert (np.abs(down(lse) / ref_lse - 1) <= 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "bf16", "i8"])
+@pytest.mark.parametrize("nats", [13.0, 15.5, 16.5, 17.5])
+def test_a_long_tail_behind_a_dominating_token(g, torch, forced, fmt, nats):  # noqa: F811
+    """A first token whose values are zero stands 13 .. 17.5 nats above 8191 others, which make the whole output.
+
+    A weight is rounded to 16 bits once.  It is at most 2^6 against the row's reference, and the largest is at least 1 of it.
+    Lifted by 2^9 it stays below fp16's 2^16, so that below 2^-14 it is rounded in steps of 2^-24, an error of
+    2^-25 2^-9 of the largest weight and less of the sum: 2^-34 sum |v| over the row's tokens.  (At 8 bits it is the weight times
+    its scale over the power of two above the largest scale that is rounded: at most twice 2^-34 of the largest value.)"""
+    L, D = 8192, 64
+    type = "bf16" if fmt == "bf16" else "f16"
+    c = Case(g, torch, [(1, L)], fmt=fmt, H=1, G=2, D=D, page=64, type=type, seed=20)
+    c.q = np.zeros_like(c.q)
+    c.q[:, :, 0] = 1.0
+    first = (c.table[0, 0], 0, 0)
+    for name, x in (("k", np.zeros((c.n_pages, 1, 64, D))), ("v", c.rng.uniform(0.5, 1.5, (c.n_pages, 1, 64, D)))):
+        if name == "k":
+            x[first + (0,)] = nats
+        else:
+            x[first] = 0
+        if fmt == "i8":
+            c.pool[name], c.scales[name] = kv.quantise(x)
+        else:
+            c.pool[name] = kv.round_to(x, fmt)
+    c.upload()
+    out, lse = c.attend(scale=1.0)
+    v = np.abs(kv.values(c.pool["v"], c.scales["v"]))
+    total = v[c.table[0]].sum((0, 1, 2)).max() if fmt != "i8" else 2 * L * v.max()
+    err, bound = error_and_bound(c, out, 1.0, np.full(c.rows, 2.0 ** -34 * total))
+    assert (err <= bound).all(), (err / bound).max()
+    ref = c.want(scale=1.0)[1]
+    assert np.abs(down(lse) - ref).max() <= 2 * D * 2.0 ** -24 * nats + 2.0 ** -20 * (1 + nats)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "bf16", "i8"])
+@pytest.mark.parametrize("base", [2.0 ** 21, 2.0 ** 22 - 2048, 2.0 ** 23 - 2048, 2.0 ** 24 - 2048, -2.0 ** 22 - 2048, -2.0 ** 24 - 2048])
+@pytest.mark.parametrize("step", [5, 14, 16])
+def test_large_scores_that_rise_tile_by_tile(g, torch, forced, fmt, base, step):  # noqa: F811
+    """Scores near the powers of two where their spacing doubles, rising with every 32 tokens: whatever the rounding of a score makes of
+    its weight, outputs are averages of the values, so they lie between their bounds (within the weights' and the output's
+    rounding)."""
+    L, D = 1024, 64
+    type = "bf16" if fmt == "bf16" else "f16"
+    c = Case(g, torch, [(1, L)], fmt=fmt, H=1, G=1, D=D, page=64, type=type, seed=26)
+    c.q = np.zeros_like(c.q)
+    c.q[0, 0, :2] = 2048, 1
+    k, v = np.zeros((c.n_pages, 1, 64, D)), c.rng.uniform(0.5, 1.5, (c.n_pages, 1, 64, D))
+    for t in range(L):
+        k[c.table[0, t // 64], 0, t % 64, :2] = base / 2048, 1800 + t // 32 * step
+    for name, x in (("k", k), ("v", v)):
+        if fmt == "i8":
+            c.pool[name], c.scales[name] = kv.quantise(x)
+        else:
+            c.pool[name] = kv.round_to(x, fmt)
+    c.upload()
+    out, lse = c.attend(scale=float(np.log(2)))
+    held, far = kv.values(c.pool["v"], c.scales["v"])[c.table[0]], 2.0 * (U[type] + U["bf16" if fmt == "bf16" else "f16"] + 2.0 ** -12)
+    assert held.min() - far <= down(out).min() and down(out).max() <= held.max() + far
+    assert np.isfinite(down(lse)).all()
