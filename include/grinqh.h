@@ -384,7 +384,9 @@ typedef struct {
  * the values (fp16, for a bf16 cache bf16).  In fp16 11 bits of it stay down
  * to 2^-23 of the row's largest weight, at an 8-bit cache to value scales 2^23
  * below the largest that the row has seen; what is below is off by at most
- * 2^-34 (2^-33 at 8 bits) of the largest.
+ * 2^-34 (2^-33 at 8 bits) of the largest.  Scores times log2 e have to stay
+ * inside fp32; of bf16 queries over an 8-bit cache, which are held as fp16
+ * times a power of two, (q . k) / max |q| has to stay under 2^112.
  * The rows' own tokens have to be in the cache already (grinqh_kv_write).
  * workspace: device, 16-byte aligned, of at least the size that
  * grinqh_attend_workspace_bytes gives for the same arguments (host only; may

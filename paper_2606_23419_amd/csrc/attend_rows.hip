@@ -114,7 +114,7 @@ void k_attend_rows(AttendArgs args) {
         const int d = I8 ? (k >> 1) * 64 + 16 * quad + 8 * (k & 1) : 32 * k + 8 * quad;
         qf[n][k] = *(const u32x4*)(qp + 2 * d);
       }
-      factor[n] = a.scale * kLog2e;
+      factor[n] = bounded(a.scale * kLog2e);
       if constexpr (I8 && TYPE == GRINQH_BF16) {
         float amax = 0;
         bool bad = false;
@@ -126,11 +126,11 @@ void k_attend_rows(AttendArgs args) {
           }
         if (bad) amax = INFINITY;
         amax = max_xor16(max_xor32(amax));
-        const int up = row_shift(amax);
+        const int up = row_shift(amax, factor[n]);
         for (int k = 0; k < KS; ++k)
           for (int e = 0; e < 4; ++e)
             qf[n][k][e] = pack2<GRINQH_F16>(ldexpf(bf2f((uint16_t)qf[n][k][e]), up), ldexpf(bf2f((uint16_t)(qf[n][k][e] >> 16)), up));
-        factor[n] = ldexpf(factor[n], -up);
+        factor[n] = bounded(ldexpf(factor[n], -up));
       }
     }
 

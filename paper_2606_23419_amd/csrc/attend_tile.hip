@@ -107,7 +107,7 @@ void k_attend_tile(AttendArgs args) {
 
     const DenseRows q = late().q;
     u32x4 qf[KS];
-    float factor = a.scale * kLog2e;
+    float factor = bounded(a.scale * kLog2e);
     {
       const char* qp = q.p + (row * q.row + head * q.head) * 2 + 16 * half;
 #pragma unroll
@@ -124,13 +124,13 @@ void k_attend_tile(AttendArgs args) {
             amax = fmaxf(amax, fabsf(x));
           }
         if (bad) amax = INFINITY;
-        const int up = row_shift(max_xor32(amax));
+        const int up = row_shift(max_xor32(amax), factor);
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             qf[k][e] = pack2<GRINQH_F16>(ldexpf(bf2f((uint16_t)qf[k][e]), up), ldexpf(bf2f((uint16_t)(qf[k][e] >> 16)), up));
-        factor = ldexpf(factor, -up);
+        factor = bounded(ldexpf(factor, -up));
       }
     }
 

@@ -115,3 +115,28 @@ def test_large_scores_that_rise_tile_by_tile(g, torch, forced, fmt, base, step):
     held, far = kv.values(c.pool["v"], c.scales["v"])[c.table[0]], 2.0 * (U[type] + U["bf16" if fmt == "bf16" else "f16"] + 2.0 ** -12)
     assert held.min() - far <= down(out).min() and down(out).max() <= held.max() + far
     assert np.isfinite(down(lse)).all()
+
+
+@pytest.mark.parametrize("power,scale", [(-120, 128 ** -0.5), (-128, 1 / 128), (-131, 1 / 128), (-80, 2.0 ** -60), (-60, 2.0 ** -149), (0, 2.0 ** -149),
+                                         (100, 2.0 ** -140)])
+def test_queries_whose_scores_vanish(g, torch, forced, power, scale):  # noqa: F811
+    """bf16 queries against an 8-bit cache, down to subnormal ones, under scales that take the scores to zero or near it:
+    plain averages of what a row sees."""
+    c = Case(g, torch, [(1, 90), (40, 200), (70, 70)], type="bf16", H=1, G=4, page=16, seed=21)
+    c.q[1:] = kv.round_bf16(c.q[1:] * 2.0 ** power)     # the first row keeps scores of its own
+    c.upload()
+    scale = float(np.float32(scale))
+    c.check(*c.attend(scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("fmt,type,power,scale", [("f16", "f16", 0, 3e38), ("bf16", "bf16", 0, 3e38), ("i8", "f16", 0, 3e38), ("i8", "bf16", 120, 2.0 ** 30)])
+def test_scores_of_zero_under_a_large_scale(g, torch, forced, fmt, type, power, scale):  # noqa: F811
+    """Queries that keys of zero meet: scores of zero, whatever the scale."""
+    c = Case(g, torch, [(1, 90), (40, 200)], fmt=fmt, type=type, H=1, G=4, page=16, seed=22)
+    c.q = kv.round_to(c.q * 2.0 ** power, type)
+    c.pool["k"] = np.zeros_like(c.pool["k"])
+    if fmt == "i8":
+        c.scales["k"] = np.zeros_like(c.scales["k"])
+    c.upload()
+    scale = float(np.float32(scale))
+    c.check(*c.attend(scale=scale), scale=scale)
