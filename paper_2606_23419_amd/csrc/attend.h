@@ -208,11 +208,11 @@ __device__ __forceinline__ uint32_t codes2(uint32_t offset_binary, uint32_t a, u
 }
 
 // Queries of a row for the products with an 8-bit cache: fp16 as they are, bf16 as fp16 times the power of
-// two that brings the row's largest magnitude to 2^14..2^15 (exact but for what lies 2^28 below it).  The scores' factor, which
+// two that brings the row's largest finite magnitude to 2^14..2^15 (exact but for what lies 2^28 below it).  The scores' factor, which
 // takes it back, stays a normal number: a row's power is held back where the factor would be under 2^-126, what that costs a score
 // is under 2^-137 of the keys' scale.  A factor of zero would make NaN of the masked scores, -inf.
 __device__ __forceinline__ int row_shift(float amax, float factor) {
-  return amax > 0 && amax < INFINITY ? min(14 - ilogbf(amax), 126 + ilogbf(factor)) : 0;
+  return amax > 0 ? min(14 - ilogbf(amax), 126 + ilogbf(factor)) : 0;
 }
 // And it is finite: zero times infinity would make NaN of scores of zero.
 __device__ __forceinline__ float bounded(float factor) { return fminf(factor, 0x1.fffffep127f); }

@@ -117,14 +117,11 @@ void k_attend_rows(AttendArgs args) {
       factor[n] = bounded(a.scale * kLog2e);
       if constexpr (I8 && TYPE == GRINQH_BF16) {
         float amax = 0;
-        bool bad = false;
         for (int k = 0; k < KS; ++k)
           for (int e = 0; e < 8; ++e) {
             const float x = bf2f((uint16_t)(qf[n][k][e >> 1] >> (16 * (e & 1))));
-            bad |= !(fabsf(x) < INFINITY);
-            amax = fmaxf(amax, fabsf(x));
+            amax = fmaxf(amax, fabsf(x) < INFINITY ? fabsf(x) : 0.0f);
           }
-        if (bad) amax = INFINITY;
         amax = max_xor16(max_xor32(amax));
         const int up = row_shift(amax, factor[n]);
         for (int k = 0; k < KS; ++k)

@@ -114,16 +114,13 @@ void k_attend_tile(AttendArgs args) {
       for (int k = 0; k < KS; ++k) qf[k] = *(const u32x4*)(qp + 32 * k);
       if constexpr (I8 && TYPE == GRINQH_BF16) {
         float amax = 0;
-        bool bad = false;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float x = bf2f((uint16_t)(qf[k][e >> 1] >> (16 * (e & 1))));
-            bad |= !(fabsf(x) < INFINITY);
-            amax = fmaxf(amax, fabsf(x));
+            amax = fmaxf(amax, fabsf(x) < INFINITY ? fabsf(x) : 0.0f);
           }
-        if (bad) amax = INFINITY;
         const int up = row_shift(max_xor32(amax), factor);
 #pragma unroll
         for (int k = 0; k < KS; ++k)

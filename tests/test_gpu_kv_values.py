@@ -140,3 +140,19 @@ def test_scores_of_zero_under_a_large_scale(g, torch, forced, fmt, type, power, 
     c.upload()
     scale = float(np.float32(scale))
     c.check(*c.attend(scale=scale), scale=scale)
+
+
+def test_infinite_queries(g, torch, forced):  # noqa: F811
+    """A channel of -inf along positive keys makes every score -inf, and the row zeros, beside finite channels far outside
+    fp16's range; one of +inf or NaN makes the row NaN."""
+    c = Case(g, torch, [(5, 90)], type="bf16", H=1, G=4, page=16, seed=23)
+    c.pool["k"][..., 0] = np.maximum(np.abs(c.pool["k"][..., 0].astype(int)), 1)
+    c.q[:, 0, 0], c.q[:, 0, 1], c.q[:, 0, 2] = -np.inf, 2.0 ** 40, -2.0 ** 40
+    c.q[:, 1, 0], c.q[:, 1, 1] = np.inf, 2.0 ** 40
+    c.q[:, 2, 5] = np.nan
+    c.upload()
+    out, lse = c.attend()
+    got, z = down(out), down(lse)
+    assert (got[:, 0] == 0).all() and (z[:, 0] == -np.inf).all()
+    assert np.isnan(got[:, 1:3]).all() and np.isnan(z[:, 1:3]).all()
+    c.check(out, lse)
