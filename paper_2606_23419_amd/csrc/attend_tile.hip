@@ -426,20 +426,15 @@ void k_attend_tile(AttendArgs args) {
         }
       }
       const float base = held == -INFINITY ? 0.0f : held;
-      // the factor 2^(kUp - ev) goes into the tokens' scales, which the wave shares: that of the largest ev,
-      // and where rows differ what is left of theirs (powers of two: exact)
-      float down = 1, fix = 1;
+      // the factor 2^(kUp - ev) goes into the tokens' scales, which the wave shares, where its rows have one ev, else into
+      // the weights: of rows whose ev lie far apart no common factor would leave all in range.  (A scale is at most 2^121.01,
+      // the largest fp32 over 127, so its product with a weight of up to 2^6 is finite.  Exact either way, but that of values
+      // under 2^-80 such a product can be subnormal and lose bits 2^-43 below the row's largest.)
+      float down = 1, own = 1;
       bool shared = true;
       if constexpr (I8) {
-        int top = __builtin_amdgcn_readfirstlane(ev);
-        shared = __all(ev == top);
-        if (!shared) {
-          top = ev;
-#pragma unroll
-          for (int x = 1; x < 32; x <<= 1) top = max(top, __shfl_xor(top, x));
-          fix = ldexpf(1.0f, min(top - ev, 127));
-        }
-        down = ldexpf(1.0f, kUp - top);
+        shared = __all(ev == __builtin_amdgcn_readfirstlane(ev));
+        (shared ? down : own) = ldexpf(1.0f, kUp - ev);
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -457,7 +452,7 @@ void k_attend_tile(AttendArgs args) {
           });
           if (!shared) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) p[e] *= fix;
+            for (int e = 0; e < 16; ++e) p[e] *= own;
           }
           if (masked) {   // a scale that is not finite stays with the rows that see it
 #pragma unroll

@@ -156,3 +156,19 @@ def test_infinite_queries(g, torch, forced):  # noqa: F811
     assert (got[:, 0] == 0).all() and (z[:, 0] == -np.inf).all()
     assert np.isnan(got[:, 1:3]).all() and np.isnan(z[:, 1:3]).all()
     c.check(out, lse)
+
+
+@pytest.mark.parametrize("power", [60, 90])
+def test_rows_of_a_chunk_whose_values_lie_far_apart(g, torch, forced, power):  # noqa: F811
+    """8-bit values of 2^-power up to the middle of a chunk and of 2^power from there: rows before it are as exact as if
+    the later tokens were not there."""
+    n, L, t0 = 70, 200, 158
+    c = Case(g, torch, [(n, L)], type="bf16", H=1, G=4, page=16, seed=24)
+    for t in range(L):
+        c.scales["v"][c.table[0, t // 16], :, t % 16] *= np.float32(2.0 ** (power if t >= t0 else -power))
+    c.upload()
+    out, _ = c.attend()
+    top = np.abs(kv.values(c.pool["v"], c.scales["v"]))[c.table[0, :(L + 15) // 16]].max((1, 3)).reshape(-1)
+    seen = np.maximum.accumulate(top)[np.arange(L - n, L)]
+    err, bound = error_and_bound(c, out, None, 2.0 ** -23 * seen)
+    assert (err <= bound).all(), (err / bound).max()
