@@ -538,7 +538,9 @@ void k_attend_tile(AttendArgs args) {
     float* lse = late().lse;
     // ---- results: lane = row, 4 channels per quad of registers
     l += __builtin_bit_cast(float, __shfl_xor(__builtin_bit_cast(int, l), 32));
-    const float inv = l == 0 ? 0.0f : (I8 ? ldexpf(1.0f, ev - kUp) : 1.0f) / l;
+    const float inv = l == 0 ? 0.0f : 1.0f / l;
+    const float back = ldexpf(1.0f, ev - kUp);   // of its own: with 1 / l it could leave fp32
+    auto result = [&](int j, int e) { return I8 ? o[j][e] * inv * back : o[j][e] * inv; };
     const float lse2 = l == 0 ? -INFINITY : m + log2f(l);
     if (w0 + (lane & 31) < all) {
       const long at = (long)row * a.heads + head;
@@ -550,7 +552,7 @@ void k_attend_tile(AttendArgs args) {
           for (int j = 0; j < VB; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              *(float4v*)(p + 32 * j + 8 * e) = float4v{o[j][4 * e] * inv, o[j][4 * e + 1] * inv, o[j][4 * e + 2] * inv, o[j][4 * e + 3] * inv};
+              *(float4v*)(p + 32 * j + 8 * e) = float4v{result(j, 4 * e), result(j, 4 * e + 1), result(j, 4 * e + 2), result(j, 4 * e + 3)};
         }
       } else {
         if (lse && half == 0) lse[at] = lse2 * kLn2;
@@ -567,7 +569,7 @@ void k_attend_tile(AttendArgs args) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *(u32x2*)(rows + (lane & 31) * STRIDE + 2 * (32 * j + 8 * e + 4 * half)) =
-              u32x2{pack2<TYPE>(o[j][4 * e] * inv, o[j][4 * e + 1] * inv), pack2<TYPE>(o[j][4 * e + 2] * inv, o[j][4 * e + 3] * inv)};
+              u32x2{pack2<TYPE>(result(j, 4 * e), result(j, 4 * e + 1)), pack2<TYPE>(result(j, 4 * e + 2), result(j, 4 * e + 3))};
       const long to = (row * out.row + head * out.head) * 2;
       wave_sync();
       constexpr int LANES = RB / 16;         // of a row

@@ -172,3 +172,29 @@ def test_rows_of_a_chunk_whose_values_lie_far_apart(g, torch, forced, power):  #
     seen = np.maximum.accumulate(top)[np.arange(L - n, L)]
     err, bound = error_and_bound(c, out, None, 2.0 ** -23 * seen)
     assert (err <= bound).all(), (err / bound).max()
+
+
+def test_the_smallest_values_of_a_long_sequence(g, torch):  # noqa: F811
+    """11 * 2^20 tokens, all but the first page 2^5 times the first's weight, of values 2^-101 throughout: the sum of the weights and
+    the values' scale both stay within fp32, their quotient would not."""
+    L, page, D = 11 << 20, 64, 64
+    desc = g.make_kv_desc(g.GRINQH_KV_I8, 1, D, page, 2)
+    cache = g.kv_cache(desc)
+    cache.k[1, 0, :, 0], cache.v[:] = 127, 64
+    cache.k_scale[:], cache.v_scale[:] = 1 / 127, 2.0 ** -107
+    table = torch.ones((1, L // page), dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    batch = g.KvBatch(table, torch.tensor([L], dtype=torch.int32, device="cuda"), torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
+    q = torch.zeros((1, 1, D), dtype=torch.bfloat16, device="cuda")
+    q[0, 0, 0] = 1
+    g.grinqh_set_option(g.GRINQH_OPT_ATTEND_KERNEL, g.GRINQH_ATTEND_TILE)
+    g.grinqh_set_option(g.GRINQH_OPT_ATTEND_SPLITS, 1)
+    try:
+        out = g.grinqh_attend(desc, cache, batch, q, scale=5 * float(np.log(2)))
+    finally:
+        g.grinqh_set_option(g.GRINQH_OPT_ATTEND_KERNEL, 0)
+        g.grinqh_set_option(g.GRINQH_OPT_ATTEND_SPLITS, 0)
+    # the output's rounding, the weights', that of exp and of the scores, and the sum's: additions of 2^10 to at most 2^28.5 a
+    # half wave, exact while the weights are 2^5 (1 +- 2^-20) and else at most 2^-18 of it each
+    bound = 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -14 + 2.0 ** -10
+    assert np.abs(down(out) / 2.0 ** -101 - 1).max() <= bound
