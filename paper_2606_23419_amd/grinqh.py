@@ -605,11 +605,18 @@ def _rows(t, dtype, name, shape):
     return _Rows(t.data_ptr(), r, h)
 
 
-def _held_for(stream, *tensors):
-    """Tensors made here and used on a stream that is not the current one stay until it is done with them."""
-    if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
+def _empty(shape, dtype, device, stream, returned=True):
+    """A tensor made here for work on `stream` (None: the current one).  Its memory is taken as that stream's: what the
+    current stream last did with it could still be under way, and the two are not ordered.  One that is returned is
+    kept from reuse until the current stream, where the caller may read it, is done with it too."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
 
 
 def grinqh_kv_write(desc: KvDesc, cache: KvCache, batch: KvBatch, k, v, stream=None) -> None:
@@ -630,11 +637,9 @@ def grinqh_kv_read(desc: KvDesc, cache: KvCache, batch: KvBatch, rows: int, dtyp
     shape = (int(rows), desc.heads, desc.head_dim)
     b = _batch_args(batch, rows)
     if k is None:
-        k = torch.empty(shape, dtype=dtype, device=cache.k.device)
-        _held_for(stream, k)
+        k = _empty(shape, dtype, cache.k.device, stream)
     if v is None:
-        v = torch.empty(shape, dtype=dtype, device=cache.k.device)
-        _held_for(stream, v)
+        v = _empty(shape, dtype, cache.k.device, stream)
     kr, vr = _rows(k, dtype, "k", shape), _rows(v, dtype, "v", shape)
     _check(lib.grinqh_kv_read(ctypes.byref(desc), ctypes.byref(c), ctypes.byref(b), _row_type(dtype, "dtype"),
                               ctypes.byref(kr), ctypes.byref(vr), _stream(stream)))
@@ -671,8 +676,7 @@ def grinqh_attend(desc: KvDesc, cache: KvCache, batch: KvBatch, q, scale=None, w
     shape = (rows, heads, desc.head_dim)
     b = _batch_args(batch, rows)
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=q.device)
-        _held_for(stream, out)
+        out = _empty(shape, q.dtype, q.device, stream)
     qr, outr = _rows(q, q.dtype, "q", shape), _rows(out, q.dtype, "out", shape)
     lp = _dev(lse, torch.float32, "lse", (rows, heads)) if lse is not None else None
     a = _attend_desc(desc, heads, _row_type(q.dtype, "q"), scale, window, sinks,
@@ -681,8 +685,7 @@ def grinqh_attend(desc: KvDesc, cache: KvCache, batch: KvBatch, q, scale=None, w
     if workspace is None:
         n = ctypes.c_size_t()
         _check(lib.grinqh_attend_workspace_bytes(ctypes.byref(desc), ctypes.byref(a), b.B, rows, ctypes.byref(n)))
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=q.device)
-        _held_for(stream, workspace)
+        workspace = _empty(n.value, torch.uint8, q.device, stream, returned=False)
     wp = _dev(workspace, torch.uint8, "workspace") if workspace.numel() else None
     _check(lib.grinqh_attend(ctypes.byref(desc), ctypes.byref(c), ctypes.byref(b), ctypes.byref(a), ctypes.byref(qr),
                              ctypes.byref(outr), lp, wp, workspace.numel(), _stream(stream)))
