@@ -254,6 +254,20 @@ def _stream(stream):
     return ctypes.c_void_p(c._cuda_getCurrentRawStream(c._cuda_getDevice()))
 
 
+def _empty(shape, dtype, device, stream, returned=True):
+    """A tensor made here for work on `stream` (None: the current one).  Its memory is taken as that stream's: what the
+    current stream last did with it could still be under way, and the two are not ordered.  One that is returned is
+    kept from reuse until the current stream, where the caller may read it, is done with it too."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def grinqh_pack(desc: LayerDesc, W=None, codes=None, scales=None, out_codes=None,
                 out_scales=None, stream=None):
     """Pack fp16 W[N, K] (RTN inside) or uint8 codes[N, K] + fp16 scales[N, K/128].
@@ -267,9 +281,9 @@ def grinqh_pack(desc: LayerDesc, W=None, codes=None, scales=None, out_codes=None
     ref = W if W is not None else codes
     dev = ref.device
     if out_codes is None:
-        out_codes = torch.empty(nc, dtype=torch.uint8, device=dev)
+        out_codes = _empty(nc, torch.uint8, dev, stream)
     if out_scales is None:
-        out_scales = torch.empty((rd.K // 128, rd.N), dtype=torch.float16, device=dev)
+        out_scales = _empty((rd.K // 128, rd.N), torch.float16, dev, stream)
     pc = _dev(out_codes, torch.uint8, "out_codes", (nc,))
     ps = _dev(out_scales, torch.float16, "out_scales", (rd.K // 128, rd.N))
     if W is not None:
@@ -300,9 +314,9 @@ def grinqh_calibrate(desc: LayerDesc, x, p_bp, per_sample=None, theta=None, stre
     n = rd.n_levels - 1
     xp = _dev(x, torch.float16, "x", (S, rd.K))
     if per_sample is None:
-        per_sample = torch.empty((S, n), dtype=torch.float64, device=x.device)
+        per_sample = _empty((S, n), torch.float64, x.device, stream, returned=False)
     if theta is None:
-        theta = torch.empty((n,), dtype=torch.float32, device=x.device)
+        theta = _empty((n,), torch.float32, x.device, stream)
     pp = _dev(per_sample, torch.float64, "per_sample", (S, n))
     tp = _dev(theta, torch.float32, "theta", (n,))
     arr = _host_array([int(v) for v in p_bp], rd.n_levels, ctypes.c_int32, "p_bp")
@@ -321,7 +335,7 @@ def grinqh_calibrate_noalloc(desc: LayerDesc, x, p_bp, theta=None, stream=None):
     n = rd.n_levels - 1
     xp = _dev(x, torch.float16, "x", (S, rd.K))
     if theta is None:
-        theta = torch.empty((n,), dtype=torch.float32, device=x.device)
+        theta = _empty((n,), torch.float32, x.device, stream)
     tp = _dev(theta, torch.float32, "theta", (n,))
     arr = _host_array([int(v) for v in p_bp], rd.n_levels, ctypes.c_int32, "p_bp")
     _check(lib.grinqh_calibrate_noalloc(ctypes.byref(rd), xp, S, arr, tp, _stream(stream)))
@@ -338,7 +352,7 @@ def grinqh_assign(desc: LayerDesc, x, mode: int, thresholds=None, counts=None, o
     B = int(x.shape[0])
     xp = _dev(x, torch.float16, "x", (B, rd.K))
     if out is None:
-        out = torch.empty((B, rd.K), dtype=torch.uint8, device=x.device)
+        out = _empty((B, rd.K), torch.uint8, x.device, stream)
     op = _dev(out, torch.uint8, "out", (B, rd.K))
     th = _thresholds(rd, thresholds) if thresholds is not None else None
     cn = _host_array([int(c) for c in counts], rd.n_levels, ctypes.c_int32, "counts") \
@@ -367,7 +381,7 @@ def grinqh_vmm(desc: LayerDesc, packed_codes, packed_scales, x, level_map, y=Non
     xp = _dev(x, torch.float16, "x", (B, rd.K))
     lp = _dev(level_map, torch.uint8, "level_map", (B, rd.K))
     if y is None:
-        y = torch.empty((B, rd.N), dtype=torch.float32, device=x.device)
+        y = _empty((B, rd.N), torch.float32, x.device, stream)
     yp = _dev(y, torch.float32, "y", (B, rd.N))
     flags = _vmm_flags(accumulate)
     _check(lib.grinqh_vmm(ctypes.byref(rd), cp, sp, xp, lp, B, yp, flags, None, 0,
@@ -389,7 +403,7 @@ def grinqh_vmm_threshold(desc: LayerDesc, packed_codes, packed_scales, x, thresh
     lo = _dev(level_map_out, torch.uint8, "level_map_out", (B, rd.K)) \
         if level_map_out is not None else None
     if y is None:
-        y = torch.empty((B, rd.N), dtype=torch.float32, device=x.device)
+        y = _empty((B, rd.N), torch.float32, x.device, stream)
     yp = _dev(y, torch.float32, "y", (B, rd.N))
     flags = _vmm_flags(accumulate)
     _check(lib.grinqh_vmm_threshold(ctypes.byref(rd), cp, sp, xp, B, _thresholds(rd, thresholds), lo,
@@ -413,7 +427,7 @@ def grinqh_vmm_topk(desc: LayerDesc, packed_codes, packed_scales, x, counts, y=N
     lo = _dev(level_map_out, torch.uint8, "level_map_out", (B, rd.K)) \
         if level_map_out is not None else None
     if y is None:
-        y = torch.empty((B, rd.N), dtype=torch.float32, device=x.device)
+        y = _empty((B, rd.N), torch.float32, x.device, stream)
     yp = _dev(y, torch.float32, "y", (B, rd.N))
     flags = _vmm_flags(accumulate)
     _check(lib.grinqh_vmm_topk(ctypes.byref(rd), cp, sp, xp, B, cn, lo, yp, flags, None, 0,
@@ -433,7 +447,7 @@ def grinqh_prefill(desc: LayerDesc, packed_codes, packed_scales, x, y=None,
     sp = _dev(packed_scales, torch.float16, "packed_scales", (rd.K // 128, rd.N))
     xp = _dev(x, torch.float16, "x", (M, rd.K))
     if y is None:
-        y = torch.empty((M, rd.N), dtype=torch.float32, device=x.device)
+        y = _empty((M, rd.N), torch.float32, x.device, stream)
     yp = _dev(y, torch.float32, "y", (M, rd.N))
     flags = GRINQH_VMM_ACCUMULATE if accumulate else 0
     _check(lib.grinqh_prefill(ctypes.byref(rd), cp, sp, xp, M, yp, flags, _stream(stream)))
@@ -474,7 +488,7 @@ def grinqh_vmm_lut(desc: LayerDesc, packed_codes, luts, x, level_map, y=None,
     xp = _dev(x, torch.float16, "x", (B, rd.K))
     mp = _dev(level_map, torch.uint8, "level_map", (B, rd.K))
     if y is None:
-        y = torch.empty((B, rd.N), dtype=torch.float32, device=x.device)
+        y = _empty((B, rd.N), torch.float32, x.device, stream)
     yp = _dev(y, torch.float32, "y", (B, rd.N))
     flags = GRINQH_VMM_ACCUMULATE if accumulate else 0
     _check(lib.grinqh_vmm_lut(ctypes.byref(rd), cp, lp, xp, mp, B, yp, flags, _stream(stream)))
@@ -496,7 +510,7 @@ def grinqh_vmm_lut_threshold(desc: LayerDesc, packed_codes, luts, x, thresholds,
     lo = _dev(level_map_out, torch.uint8, "level_map_out", (B, rd.K)) \
         if level_map_out is not None else None
     if y is None:
-        y = torch.empty((B, rd.N), dtype=torch.float32, device=x.device)
+        y = _empty((B, rd.N), torch.float32, x.device, stream)
     yp = _dev(y, torch.float32, "y", (B, rd.N))
     flags = GRINQH_VMM_ACCUMULATE if accumulate else 0
     _check(lib.grinqh_vmm_lut_threshold(ctypes.byref(rd), cp, lp, xp, B, _thresholds(rd, thresholds), lo, yp,
@@ -603,20 +617,6 @@ def _rows(t, dtype, name, shape):
     if d != 1:
         raise ValueError(f"{name} must be contiguous along head_dim")
     return _Rows(t.data_ptr(), r, h)
-
-
-def _empty(shape, dtype, device, stream, returned=True):
-    """A tensor made here for work on `stream` (None: the current one).  Its memory is taken as that stream's: what the
-    current stream last did with it could still be under way, and the two are not ordered.  One that is returned is
-    kept from reuse until the current stream, where the caller may read it, is done with it too."""
-    torch = _torch()
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    if returned:
-        t.record_stream(torch.cuda.current_stream(device))
-    return t
 
 
 def grinqh_kv_write(desc: KvDesc, cache: KvCache, batch: KvBatch, k, v, stream=None) -> None:
