@@ -8,6 +8,7 @@ embedding and the MLP are left out.
     python examples/attention_block.py [--window 256 --sinks 4]
 """
 import argparse
+import math
 import os
 import sys
 
@@ -103,7 +104,10 @@ def run(lengths=(300, 77, 1), steps=16, window=0, sinks=0):
         kept[s].append(qkv[:, HEADS:].clone())
         kv = torch.cat(kept[s])
         ref = plain(qkv[:, :HEADS], kv[:, :KV_HEADS], kv[:, KV_HEADS:], window, sinks)
-        worst = max(worst, ((a.float() - ref).norm() / ref.norm()).item())
+        error = ((a.float() - ref).norm() / ref.norm()).item()
+        if not math.isfinite(error):     # max() would pass over a NaN
+            raise FloatingPointError(f"attention of sequence {s}, {kv.shape[0]} tokens, is not finite")
+        worst = max(worst, error)
 
     y, qkv, a = block.prompts(x, lengths)
     for s, (rows, att) in enumerate(zip(qkv.split(lengths), a.split(lengths))):
