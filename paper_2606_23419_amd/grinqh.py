@@ -106,7 +106,8 @@ class _Rows(ctypes.Structure):
 
 
 # The arrays of a cache and of a batch, as grinqh.h lays them out.  They keep the C structure made of them, which is
-# used again as long as it was checked against the same descriptor and every array is where and as it was.
+# used again as long as it was checked against the same descriptor and every array is where and as it was: address, shape,
+# type, on a device, contiguous.
 class KvCache(collections.namedtuple("KvCache", "k v k_scale v_scale")):
     pass
 
@@ -567,7 +568,7 @@ def kv_cache(desc: KvDesc, device="cuda") -> KvCache:
 
 
 def _cache_args(desc, cache):
-    at = [(t.data_ptr(), t.shape, t.stride()) if t is not None else None for t in cache]
+    at = [(t.data_ptr(), t.shape, t.dtype, t.is_cuda, t.is_contiguous()) if t is not None else None for t in cache]
     key = (desc.format, desc.heads, desc.head_dim, desc.page, desc.n_pages, at)
     kept = cache.__dict__.get("_args")
     if kept is not None and kept[0] == key:
@@ -587,7 +588,7 @@ def _cache_args(desc, cache):
 
 
 def _batch_args(batch, rows):
-    key = (int(rows), [(t.data_ptr(), t.shape, t.stride()) for t in batch])
+    key = (int(rows), [(t.data_ptr(), t.shape, t.dtype, t.is_cuda, t.is_contiguous()) for t in batch])
     kept = batch.__dict__.get("_args")
     if kept is not None and kept[0] == key:
         return kept[1]

@@ -31,3 +31,18 @@ def test_memory_still_in_use_on_the_current_stream(g, torch):  # noqa: F811
         torch.cuda.synchronize()
         assert self_equal(torch, out, want)
         assert self_equal(torch, k, rows[0]) and self_equal(torch, v, rows[1])
+
+
+def test_arrays_of_another_type_under_a_handle(g, torch):  # noqa: F811
+    """A handle's checked arguments are not used again for arrays that have changed their type in place."""
+    c = Case(g, torch, [(4, 9)], fmt="f16", page=16).upload()
+    q = up(torch, c.q, "f16")
+    g.grinqh_attend(c.desc, c.cache, c.batch, q)
+    c.cache.v.data = c.cache.v.data.view(torch.bfloat16)
+    with pytest.raises(TypeError):
+        g.grinqh_attend(c.desc, c.cache, c.batch, q)
+    c.cache.v.data = c.cache.v.data.view(torch.float16)
+    g.grinqh_attend(c.desc, c.cache, c.batch, q)
+    c.batch.seq_lens.data = c.batch.seq_lens.data.view(torch.float32)
+    with pytest.raises(TypeError):
+        g.grinqh_attend(c.desc, c.cache, c.batch, q)
