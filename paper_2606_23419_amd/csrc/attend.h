@@ -11,8 +11,8 @@ typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bhalf2 __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
-
-
+// Four scales, whose arrays are 4-byte aligned (such a load needs no more).
+typedef float float4s __attribute__((ext_vector_type(4), aligned(4)));
 
 // Results of the splits of a block of rows that has more than one (Span::splits): o [split][row * heads + head][D],
 // normalised, and lse (base 2) [split][row * heads + head]; o is not written where lse is -inf.

@@ -205,8 +205,8 @@ void k_attend_rows(AttendArgs args) {
       if constexpr (I8 && !SMALL) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          kst[t] = load_global<float4v>((const char*)ksp[t] + (uint32_t)(16 * quad));
-          vst[t] = load_global<float4v>((const char*)vsp[t] + (uint32_t)(16 * quad));
+          kst[t] = load_global<float4s>((const char*)ksp[t] + (uint32_t)(16 * quad));
+          vst[t] = load_global<float4s>((const char*)vsp[t] + (uint32_t)(16 * quad));
         }
       }
     };

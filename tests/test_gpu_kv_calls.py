@@ -3,7 +3,8 @@ are not written."""
 import numpy as np
 import pytest
 
-from test_gpu_kv import Case, g, self_equal, torch, up  # noqa: F401 (fixtures)
+from oracle import kv_oracle as kv
+from test_gpu_kv import Case, down, forced, g, rows_of, self_equal, torch, up  # noqa: F401 (fixtures)
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +47,27 @@ def test_arrays_of_another_type_under_a_handle(g, torch):  # noqa: F811
     c.batch.seq_lens.data = c.batch.seq_lens.data.view(torch.float32)
     with pytest.raises(TypeError):
         g.grinqh_attend(c.desc, c.cache, c.batch, q)
+
+
+@pytest.mark.parametrize("page", [8, 64])
+@pytest.mark.parametrize("type", ["f16", "bf16"])
+def test_scales_aligned_to_four_bytes(g, torch, forced, type, page):  # noqa: F811
+    """The scales of an 8-bit cache start one word into their memory, as an allocator's slices may."""
+    c = Case(g, torch, [(1, 77), (40, 300), (90, 90)], type=type, H=3, G=2, page=page, seed=30).upload()
+
+    def moved(t):
+        wide = torch.full((t.numel() + 2,), 5.0, device="cuda")
+        wide[1:-1] = t.view(-1)
+        assert wide[1:-1].data_ptr() % 16 == 4
+        return wide[1:-1].view(t.shape)
+
+    c.cache = c.cache._replace(k_scale=moved(c.cache.k_scale), v_scale=moved(c.cache.v_scale))
+    c.check(*c.attend())
+    x = {n: rows_of(torch, np.random.default_rng(31), c.rows, 3, 128, type, "plain") for n in "kv"}
+    g.grinqh_kv_write(c.desc, c.cache, c.batch, x["k"][1], x["v"][1])
+    got = g.grinqh_kv_read(c.desc, c.cache, c.batch, c.rows, dtype=torch.float32)
+    for n, t in zip("kv", got):
+        kv.write(c.pool[n], c.scales[n], "i8", c.table, c.lens, c.offsets, x[n][0])
+        ref, _ = kv.read(c.pool[n], c.scales[n], c.table, c.lens, c.offsets, c.rows)
+        assert np.array_equal(down(t), ref.astype(np.float32).astype(np.float64))
+        assert np.array_equal(down(getattr(c.cache, n + "_scale")), c.scales[n].astype(np.float64))
