@@ -298,9 +298,12 @@ GRINQH_API int grinqh_vmm_lut_threshold(const grinqh_layer_desc* desc, const voi
  * is in place t % page of page block_table[b][t / page].
  * The batch's arrays live on the device and are read by the kernels, so a
  * captured graph follows what later steps write there.  What the host cannot
- * check is bounded in the kernels: offsets are clamped to 0..rows and to
- * ascending order, lengths to 0..min(table_width * page, 2^30); rows of no
- * sequence are not touched; memory of a page id outside 0..n_pages-1 is never accessed. */
+ * check is bounded in the kernels: offsets are clamped to 0..rows, a sequence
+ * that ends before it starts has no rows, lengths are clamped to
+ * 0..min(table_width * page, 2^30); rows of no sequence are not touched; memory
+ * of a page id outside 0..n_pages-1 is never accessed.  Offsets have to ascend:
+ * where they do not, nothing outside the arrays is touched, but which of the
+ * rows between are done, and for which sequence, is not defined. */
 enum { GRINQH_F16 = 0, GRINQH_BF16 = 1, GRINQH_F32 = 2 };            /* types of dense rows */
 enum { GRINQH_KV_F16 = 0, GRINQH_KV_BF16 = 1, GRINQH_KV_I8 = 2 };    /* formats of the cache */
 

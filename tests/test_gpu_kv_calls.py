@@ -71,3 +71,36 @@ def test_scales_aligned_to_four_bytes(g, torch, forced, type, page):  # noqa: F8
         ref, _ = kv.read(c.pool[n], c.scales[n], c.table, c.lens, c.offsets, c.rows)
         assert np.array_equal(down(t), ref.astype(np.float32).astype(np.float64))
         assert np.array_equal(down(getattr(c.cache, n + "_scale")), c.scales[n].astype(np.float64))
+
+
+@pytest.mark.parametrize("fmt", ["i8", "f16", "bf16"])
+@pytest.mark.parametrize("offsets,lens", [
+    ([2, 5, 7], [6, 9]),                    # two rows before the first sequence, two behind the last
+    ([0, 0, 3, 3, 3, 9], [4, 11, 2, 0, 8]),  # sequences of no rows at either end of others
+    ([9, 9, 9], [6, 9]),
+    ([-4, 3, 100], [6, 12]),                # clamped to the rows
+    ([5, 5, 8, 8], [3, 7, 10]),
+])
+def test_only_the_rows_of_sequences_are_written(g, torch, fmt, offsets, lens):  # noqa: F811
+    """The whole cache after a write of new values, bit for bit, and rows read back beside rows that are left as they were."""
+    rows, H, D = 9, 2, 64
+    c = Case(g, torch, [(0, 12)] * len(lens), fmt=fmt, H=H, G=1, D=D, page=4, seed=32)
+    c.offsets, c.lens, c.rows = np.array(offsets, np.int32), np.array(lens, np.int32), rows
+    c.upload()
+    rng = np.random.default_rng(33)
+    x = {n: rows_of(torch, rng, rows, H, D, "f16", "plain", 2.0) for n in "kv"}
+    g.grinqh_kv_write(c.desc, c.cache, c.batch, x["k"][1], x["v"][1])
+    for n in "kv":
+        before = c.pool[n].copy()
+        kv.write(c.pool[n], c.scales[n], fmt, c.table, c.lens, c.offsets, x[n][0])
+        assert np.array_equal(down(getattr(c.cache, n)), c.pool[n].astype(np.float64))
+        if fmt == "i8":
+            assert np.array_equal(down(getattr(c.cache, n + "_scale")), c.scales[n].astype(np.float64))
+        taken = sum(min(k, L) for _, k, L in kv.sequences(c.offsets, c.lens, c.width, c.page, rows))
+        assert (before != c.pool[n]).any((1, 3)).sum() == taken
+    k = torch.full((rows, H, D), 5.0, device="cuda")
+    v = k.clone()
+    g.grinqh_kv_read(c.desc, c.cache, c.batch, rows, dtype=torch.float32, k=k, v=v)
+    for n, t in (("k", k), ("v", v)):
+        ref, written = kv.read(c.pool[n], c.scales[n], c.table, c.lens, c.offsets, rows)
+        assert np.array_equal(down(t)[written], ref[written].astype(np.float32).astype(np.float64)) and (down(t)[~written] == 5).all()
