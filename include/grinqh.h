@@ -370,7 +370,9 @@ typedef struct {
                         tokens before it */
   int32_t sinks;     /* first tokens of a sequence that stay visible behind the window */
   int32_t max_rows;  /* upper estimates of the rows and of the length of one sequence: they
-                        shape the launch and never change what is computed */
+                        shape the launch and never change what is computed.  Loose ones
+                        cost time: 32 tokens decoded after up to 8190 others take 66 us with
+                        exact ones, 193 us with max_len = 131072, 387 us with max_rows = 32 */
   int32_t max_len;
 } grinqh_attend_desc;
 
@@ -380,7 +382,8 @@ typedef struct {
  * over the visible t.  A row that sees nothing (or only scores of -inf) is 0.
  * lse (fp32 [rows][heads], contiguous, or NULL) gets m + log sum_t exp(s_t - m),
  * -inf for such a row.  What a row does not see never reaches it, infinities
- * and NaN included; a visible token whose page id is out of range makes the
+ * and NaN included; a value that it sees and that is not finite makes its
+ * channel infinite or NaN; a visible token whose page id is out of range makes the
  * row NaN, pages that no row sees may have any id.
  * Precision: scores, statistics and sums in fp32; exp(s_t - m), at an 8-bit
  * cache times the value's scale, is rounded to 16 bits for the product with

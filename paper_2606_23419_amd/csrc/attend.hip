@@ -92,9 +92,10 @@ AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
   const int forced = option(&Options::attend_kernel), forced_splits = option(&Options::attend_splits);
   const long n = std::min(a.max_rows, rows), R = n * a.G;
   // R rows of a kv head share its K and V.  Up to 32 of them are one workgroup's in k_attend_rows, the next read the cache
-  // again, from L2 at first.  8 bits, rows kernel against tile kernel, us: R = 64 over 8190 tokens of 1 sequence 26 : 36, of
-  // 4 42 : 58; 500 tokens of 4 17 : 33; 2000 of 32 97 : 98; 16 bits, 8190 of 8 91 : 102.  R = 128: 34 : 39, 60 : 66,
-  // 19 : 34, 182 : 101, 214 : 110.
+  // again, from L2 at first.  8 bits, rows kernel against tile kernel, us: R = 64 over 8190 tokens of 1 sequence 27 : 37, of
+  // 4 44 : 59; 500 tokens of 4 17 : 34; 2000 of 32 101 : 98; 16 bits, 8190 of 8 90 : 102.  R = 128: 34 : 39, 62 : 66,
+  // 19 : 34, 188 : 100, 212 : 110.  Past 64 rows it depends on the number of sequences, which the rule does not look at: few
+  // short ones of 65 to 128 rows pay up to 1.8 times.
   p.tile = forced ? forced != GRINQH_ATTEND_ROWS : R > 64;
   p.nb = R > 16 ? 2 : 1;
   const long per_block = p.tile ? 256 : 16 * p.nb, tile = p.tile ? 64 : 32;

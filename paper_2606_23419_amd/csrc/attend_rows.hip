@@ -14,9 +14,12 @@
 // The next tile's K is loaded while the softmax runs, its V behind the second product.
 //
 // Bound by memory: every visible K and V row is read once.  One token over 131072 tokens of an 8-bit cache, 8 kv heads
-// of 128 (277 MB): 44.6 us in this kernel, 6.2 TB/s where a plain read of 2 GiB reaches 6.9, and 4.8 us joining 64
+// of 128 (277 MB): 44.4 us in this kernel, 6.2 TB/s where a plain read of 2 GiB reaches 6.9, and 5.1 us joining 64
 // parts; 32 sequences up to 8191 tokens, bf16 rows (269 MB): 51 and 5 us.  A part of a few tiles is a chain of latencies
-// (page id, loads, two products): one token after 76 takes 6.1 us, of which its 0.2 MB are nothing.
+// (page id, loads, two products): one token after 76 takes 6.2 us, of which its 0.2 MB are nothing.  With NB = 2 it is far
+// from that bound (64 rows of a kv head over 8190 tokens of 4 sequences, 69 MB: 43 us): 33 rows and more are two workgroups
+// that each read the cache, and at D = 128 over a 16-bit one the kernel needs more than 256 registers and keeps 12 to 15
+// values in scratch.
 #include "attend.h"
 
 namespace grinqh {

@@ -7,19 +7,22 @@
 //     exchange of the two half waves, and the rescaling factor of O^T is the lane's own.
 //   - the weights come out of the first product where the second wants them: its contraction is over tokens in
 //     any order, and ds_read_b64_tr_b16 hands V over in the order of S^T's registers, channel per lane.
-//   - 16-byte chunks of K's and V's rows are swizzled in LDS so that neither read conflicts.
+//   - 16-byte chunks of K's and V's rows are swizzled in LDS so that neither read conflicts.  (The rows that codes become are
+//     written every second chunk at a time, which does: 0.15 of the cycles that LDS is busy.)
 // 16-bit rows go to LDS directly; int8 rows pass through registers and become fp16 codes (exact), K's scales
 // multiply the scores and V's the weights, each lane holding the scale of one token that the multiplication
 // broadcasts by DPP.  Tiles are copied several slots ahead, and the waves run in two halves half a tile apart: one
 // half's products meet the other's softmax.
 //
-// Bound by the vector unit beside the matrix cores: 4 D operations per row and visible token in products of 32 cycles, and
-// with each at 8 bits about nine other vector instructions (scales, maximum, exponential, sum, packing, codes to fp16).
-// 4096 rows of 32 heads behind 32768 tokens of an 8-bit cache (2.34 Tflop): 2.68 .. 2.83 ms, 825 .. 870 TFLOP/s, where a library
-// product of 8192^3 reaches 1200; the products hold their pipe 0.36 of the time.  16-bit caches pay for the staging (page addresses,
-// issue of the copies, a workgroup's first tile): without it in the loop they came to 1300; copies spread among the products were faster at D = 64 (541 -> 472 us) and slower
-// at D = 128, so they stand together.  A call of one tile takes 12 us, and 1.8 to 2.2 us go with every further one: a prompt
-// of 2048 tokens from its start (34 Gflop, 8 kv heads of 4) is 256 workgroups of 4 to 32 tiles, and the longest makes its 74 us.
+// 4096 rows of 32 heads behind 32768 tokens of an 8-bit cache (2.34 Tflop): 2.69 .. 2.84 ms, 825 .. 870 TFLOP/s, where a library
+// product of 8192^3 reaches 1200.  Neither pipe is full: a SIMD takes 89 cycles a product, of which the product holds its pipe
+// 32, and about nine other vector instructions that go with it at 8 bits (scales, maximum, exponential, sum, packing, codes to
+// fp16) take 38 to 50.  That is near the sum of the two, which the halves of the workgroup are there to overlap; waves wait in a
+// third of their cycles, and what for is not known.  16-bit caches pay for the staging (page addresses, issue of the copies, a
+// workgroup's first tile): without it in the loop they came to 1300; copies spread among the products were faster at D = 64
+// (541 -> 472 us) and slower at D = 128, so they stand together.  A call of one tile takes 12 us, and 1.8 to 2.2 us go with every
+// further one: a prompt of 2048 tokens from its start (34 Gflop, 8 kv heads of 4) is 256 workgroups of 4 to 32 tiles, and the
+// longest makes its 76 us.
 #include "attend.h"
 
 namespace grinqh {

@@ -668,7 +668,8 @@ def grinqh_attend(desc: KvDesc, cache: KvCache, batch: KvBatch, q, scale=None, w
     """out [rows, heads, head_dim] of q's type: attention of the rows q over the cache (see grinqh.h).
 
     max_rows and max_len bound the rows and the length of one sequence from above; they shape the launch only, and
-    default to the bounds that the shapes give.  lse (fp32 [rows, heads]) is written if it is passed."""
+    default to the bounds that the shapes give, all rows in one sequence and a full table.  Pass what is known: a decode
+    step of many sequences with max_rows=1 is several times faster than with the default.  lse (fp32 [rows, heads]) is written if it is passed."""
     torch = _torch()
     c = _cache_args(desc, cache)
     if q.dim() != 3:
