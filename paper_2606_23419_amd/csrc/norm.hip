@@ -148,54 +148,101 @@ __device__ __forceinline__ float row_reduce(float x, float* lds) {
   }
   return x;
 }
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// The waves' two sums come back one to a lane, which meet in the order of a tree.
+template <int WAVES>
+__device__ __forceinline__ void row_sums(float* x, float* y, float* lds) {
+#pragma unroll
+  for (int s = 32; s; s >>= 1) { *x += __shfl_xor(*x, s); *y += __shfl_xor(*y, s); }
+  if constexpr (WAVES > 1) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();                         // the last reduction has been read
+    if ((threadIdx.x & 63) == 0) { lds[2 * wave] = *x; lds[2 * wave + 1] = *y; }
+    __syncthreads();
+    static_assert(WAVES == 4 || WAVES == 8 || WAVES == 16);
+    auto meet = [](float v) {
+      v = add_dpp<0x4e>(add_dpp<0xb1>(v));   // quad_perm: the neighbour, then the other two
+      if constexpr (WAVES >= 8) v = add_dpp<0x141>(v);    // row_half_mirror
+      if constexpr (WAVES == 16) v = add_dpp<0x140>(v);   // row_mirror
+      return v;
+    };
+    const int from = 2 * (threadIdx.x & (WAVES - 1));
+    *x = meet(lds[from]);
+    *y = meet(lds[from + 1]);
+  }
+}
 
 // v becomes its norm, weight and bias not yet applied.  Channels from n on are 0 and stay out of the sums.
+// LAYER takes its mean off in two parts: the sum's, m, which is off by its roundings, and the mean r of what that leaves, so the variance
+// is mean((v - m)^2) - r^2.  With the first alone a row of one value would be 1 or -1 throughout wherever m is not that value.  Of equal
+// values v - m is exact and so is the sum of a few units in the last place; r is a quotient, not a product with 1 / n, so nothing
+// is left.  Where r is no small part of what is left, the centred squares are summed once more.
 template <int LANES, int NV, int WAVES>
 __device__ __forceinline__ void normalise(int kind, float eps, int n, int lane, float (*v)[8], float* lds) {
   const float inv_n = 1.0f / n;
-  auto in = [&](int i, int j) { return 8 * (i * LANES + lane) + j < n; };
-  auto spread = [&](float up, float* mean) {  // of up v
-    *mean = 0;
-    if (kind == GRINQH_NORM_LAYER) {
-      float s = 0;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s += v[i][j] * up;
-      *mean = row_reduce<WAVES, false>(s, lds) * inv_n;
-    }
-    float s = 0;
+  float mean, rest, factor;
+  // f(t) of the channels' t = v - mean - less, 0 from n on.  (Behind the assembly nothing that another pass made is kept: registers
+  // are scarce.)
+  auto centred = [&](float less, auto f) __attribute__((always_inline)) {
+    int here = n - 8 * lane;
+    float m = mean;
+    asm volatile("" : "+v"(here), "+v"(m));
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float t = kind == GRINQH_NORM_LAYER ? (in(i, j) ? v[i][j] * up - *mean : 0.0f) : v[i][j] * up;
-        s += t * t;
-      }
+      for (int j = 0; j < 8; ++j) f(v[i][j], 8 * i * LANES + j < here ? v[i][j] - m - less : 0.0f);
+  };
+  auto spread = [&]() __attribute__((always_inline)) {
+    float s = 0;
+    mean = rest = 0;
+    if (kind != GRINQH_NORM_LAYER) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += v[i][j] * v[i][j];
+      return row_reduce<WAVES, false>(s, lds) * inv_n;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += v[i][j];
+    mean = row_reduce<WAVES, false>(s, lds) * inv_n;
+    float left = 0;
+    s = 0;
+    centred(0.0f, [&](float, float t) { left += t; s += t * t; });
+    row_sums<WAVES>(&left, &s, lds);
+    rest = left / n;
+    const float square = s * inv_n;
+    if (!(rest * rest > square * 0x1p-6f)) return square - rest * rest;
+    s = 0;
+    centred(rest, [&](float, float t) { s += t * t; });
     return row_reduce<WAVES, false>(s, lds) * inv_n;
   };
-  float mean, up = 1, factor;
-  const float ms = spread(1.0f, &mean), var = ms + eps;
+  const float var = spread() + eps;
   if (var >= 0x1p-100f && var < INFINITY) {
     factor = 1.0f / sqrtf(var);
   } else {
     // squares, or sums, that have left fp32's range, in either direction: the row times a power of two that brings its largest
-    // magnitude to 1..2, which the factor takes back
+    // magnitude to 1..2, or eps times the power's square, which is under the root then, to under 2^127 (where it outweighs all squares)
     float top = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[i][j]));
     top = row_reduce<WAVES, true>(top, lds);
-    const int e = top > 0 && top < INFINITY ? min(-ilogbf(top), 126) : 0;
-    up = ldexpf(1.0f, e);
-    const double s = spread(up, &mean);
-    factor = (float)(1.0 / sqrt(s + ldexp((double)eps, 2 * e)));   // of up v: sqrt(s up^-2 + eps) up
+    int e = top > 0 && top < INFINITY ? min(-ilogbf(top), 126) : 0;
+    if (eps > 0) e = min(e, (126 - ilogbf(eps)) >> 1);
+    const float up = ldexpf(1.0f, e);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= up;
+    factor = 1.0f / sqrtf(spread() + ldexpf(eps, 2 * e));
   }
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = in(i, j) ? (v[i][j] * up - mean) * factor : 0.0f;
+  centred(rest, [&](float& to, float t) { to = t * factor; });
 }
 
 template <int LANES, int NV>
@@ -218,12 +265,12 @@ __device__ __forceinline__ void scale_and_shift(const char* weight, const char* 
   }
 }
 
-// WAVES waves take a row, NV pieces of 8 channels a lane; with one wave a row a workgroup takes four.  With eight waves a SIMD, which
-// cost a few registers, rows of 5001 take 0.82 to 0.92 of the time that seven take and 16384 channels 0.93.
+// WAVES waves take a row, NV pieces of 8 channels a lane; with one wave a row a workgroup takes four.  With eight waves a SIMD, whose 64
+// registers suffice without scratch, rows of 5001 take 0.82 to 0.92 of the time that seven take and 16384 channels 0.93.
 template <int WAVES, int NV>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) __attribute__((amdgpu_waves_per_eu(NV <= 2 ? 8 : 4))) void k_norm(Norm a) {
   constexpr int LANES = 64 * WAVES;
-  __shared__ float lds[WAVES];
+  __shared__ float lds[2 * WAVES];
   const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
   const long row = WAVES == 1 ? (long)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (row >= a.rows) return;
