@@ -240,7 +240,8 @@ __device__ __forceinline__ void normalise(int kind, float eps, int n, int lane, 
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] *= up;
-    factor = 1.0f / sqrtf(spread() + ldexpf(eps, 2 * e));
+    const float root = spread() + ldexpf(eps, 2 * e);
+    factor = root == 0 && eps > 0 ? 0.0f : 1.0f / sqrtf(root);   // one value, whose eps is lost here: zeros times anything finite
   }
   centred(rest, [&](float& to, float t) { to = t * factor; });
 }

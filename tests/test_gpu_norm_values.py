@@ -64,3 +64,35 @@ def test_values_close_together_far_from_zero(g, torch, n, apart, eps):  # noqa: 
         far = np.abs(x.cpu().double().numpy() - want) - bound
         assert (far <= 0).all(), (far.max(), np.unravel_index(far.argmax(), far.shape))
     assert np.abs(want - step.norm(None, ref, pre="layer", eps=eps)[1]).max() <= 1e-6   # the oracle's mean in float64 does as well
+
+
+@pytest.mark.parametrize("n", [1, 41, 777, 4096, 5001, 16385])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("eps", [1e-5, 1e-32, 1e-38, 1e-44, 3e38])
+def test_equal_values_of_any_size_leave_nothing(g, torch, n, kind, eps):  # noqa: F811
+    """eps > 0: the root is that of eps, however far below the values' square it lies."""
+    sizes = [0.0, 2.0 ** -149, -1e-40, 2.0 ** -60, 1.7e-20, -2.0 ** 65, 1.3e20, 2.0 ** 125, -2.0 ** 125, 3e38, 5.0]
+    t = torch.tensor(sizes, device="cuda").to(getattr(torch, kind))[:, None].expand(len(sizes), n).contiguous()
+    weight, bias = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    for x in both(g, t, eps):
+        assert (x == 0).all(), sizes[int((x != 0).any(-1).nonzero()[0])]
+    for x in both(g, t, eps, weight=weight, bias=bias):
+        assert torch.equal(x, bias.to(x.dtype).expand_as(x))
+
+
+@pytest.mark.parametrize("size,eps", [(2.0 ** -60, 1e-32), (1e-38, 1e-32), (1e-42, 1e-32), (1e-38, 1e-44), (1e-20, 1e-38), (1e30, 1e-38), (3e37, 3e38), (1e19, 3e38)])
+@pytest.mark.parametrize("n", [41, 5001])
+def test_small_and_large_eps(g, torch, size, eps, n):  # noqa: F811
+    """eps beside squares that leave fp32's range: rows of x in fp32, down to its subnormal numbers."""
+    rng = np.random.default_rng(n)
+    v = (rng.uniform(-1, 1, (3, n)) * size).astype(np.float32)
+    t, ref, eps = torch.from_numpy(v).cuda(), v.astype(np.float64), float(np.float32(eps))
+    for kind, name in ((g.GRINQH_NORM_RMS, "rms"), (g.GRINQH_NORM_LAYER, "layer")):
+        x = g.grinqh_norm(None, t, pre=kind, eps=eps, x_dtype=torch.float32)[1].cpu().double().numpy()
+        want = step.norm(None, ref, pre=name, eps=eps)[1]
+        # a centred value is off by a step of the values' mean, at least 2^-149 (and as much when the row is scaled), x by factor times that
+        c = ref - ref.mean(-1, keepdims=True) if name == "layer" else ref
+        factor = 1 / np.sqrt((c * c).mean(-1, keepdims=True) + eps)
+        e = (S + 4 * U) * np.abs(ref).mean(-1, keepdims=True) + 3 * U * np.abs(c) + 2.0 ** -147 if name == "layer" else 0.0
+        whole = np.sqrt((e * e).mean(-1, keepdims=True)) * factor if name == "layer" else 0.0
+        assert (np.abs(x - want) <= factor * e + np.abs(want) * (F + whole) + 2.0 ** -149).all()
