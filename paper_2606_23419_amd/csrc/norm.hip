@@ -273,7 +273,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) __attribute__((amdgp
   constexpr int LANES = 64 * WAVES;
   __shared__ float lds[2 * WAVES];
   const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
-  const long row = WAVES == 1 ? (long)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const long block = (long)blockIdx.y * gridDim.x + blockIdx.x, row = WAVES == 1 ? block * 4 + (threadIdx.x >> 6) : block;
   if (row >= a.rows) return;
   float v[NV][8];
   Pieces<NV> ry, rh;
@@ -315,8 +315,10 @@ void launch_norm(const Norm& a, hipStream_t s) {
   const int pieces = (a.n + 7) / 8;
   auto go = [&](auto waves, auto nv) {
     constexpr int W = decltype(waves)::value, NV = decltype(nv)::value;
-    if (W == 1) k_norm<W, NV><<<(a.rows + 3) / 4, 256, 0, s>>>(a);
-    else k_norm<W, NV><<<a.rows, 64 * W, 0, s>>>(a);
+    // an axis of the grid has less than 2^32 threads: 2^20 workgroups and less, and the rest along the other one
+    const int threads = W == 1 ? 256 : 64 * W, blocks = W == 1 ? (a.rows + 3) / 4 : a.rows;
+    const int y = (blocks + (1 << 20) - 1) >> 20, x = (blocks + y - 1) / y;
+    k_norm<W, NV><<<dim3(x, y), threads, 0, s>>>(a);
   };
   using std::integral_constant;
   if (pieces <= 64) go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
