@@ -276,7 +276,8 @@ __global__ __launch_bounds__(kRowThreads) void k_kv_read(KvCache c, KvBatch b, D
 template <int D, int FORMAT, int TYPE>
 static void launch_rows(bool write, const KvCache& c, const KvBatch& b, const DenseRows& k, const DenseRows& v, hipStream_t s) {
   // one pass of kItems pieces per thread where a row's heads allow it
-  const int per_pass = kRowThreads * kItems / (c.H * (D / 8)), tokens = per_pass < 1 ? 1 : per_pass < kRowThreads ? per_pass : kRowThreads;
+  const int per_pass = kRowThreads * kItems / (c.H * (D / 8)), least = (b.rows + (1 << 22) - 1) >> 22;   // the grid has less than 2^32 threads
+  const int tokens = per_pass < least ? least : per_pass < kRowThreads ? per_pass : kRowThreads;
   const dim3 grid((unsigned)((b.rows + tokens - 1) / tokens), 2);
   if (write) k_kv_write<D, FORMAT, TYPE><<<grid, kRowThreads + 64, 0, s>>>(c, b, k, v, tokens);
   else k_kv_read<D, FORMAT, TYPE><<<grid, kRowThreads, 0, s>>>(c, b, k, v, tokens);
