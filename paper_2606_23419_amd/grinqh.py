@@ -554,7 +554,14 @@ def grinqh_stream_read(src, sink, stream=None):
 
 
 # ------------------------------------------ key/value cache and attention --
+def _fits(*numbers):
+    """Raises for what the interface's 32-bit integers cannot hold: ctypes would pass its low bits."""
+    if max(numbers) > 0x7fffffff or min(numbers) < -0x80000000:
+        raise ValueError(f"{next(n for n in numbers if not -0x80000000 <= n <= 0x7fffffff)} does not fit 32 bits")
+
+
 def make_kv_desc(format: int, heads: int, head_dim: int, page: int, n_pages: int) -> KvDesc:
+    _fits(format, heads, head_dim, page, n_pages)
     return KvDesc(int(format), int(heads), int(head_dim), int(page), int(n_pages))
 
 
@@ -630,6 +637,7 @@ def _batch_args(batch, rows):
     if batch.seq_lens.dim() != 1 or batch.block_table.dim() != 2:
         raise ValueError("seq_lens must have one axis and block_table two")
     B, width = int(batch.seq_lens.shape[0]), int(batch.block_table.shape[1])
+    _fits(B, width, rows)
     b = _KvBatch(_dev(batch.block_table, torch.int32, "block_table", (B, width)),
                  _dev(batch.seq_lens, torch.int32, "seq_lens"),
                  _dev(batch.row_offsets, torch.int32, "row_offsets", (B + 1,)), B, width, int(rows))
@@ -684,6 +692,7 @@ def grinqh_kv_read(desc: KvDesc, cache: KvCache, batch: KvBatch, rows: int, dtyp
 def _attend_desc(desc, heads, type, scale, window, sinks, max_rows, max_len):
     if scale is None:
         scale = float(desc.head_dim) ** -0.5
+    _fits(heads, window, sinks, max_rows, max_len)
     return AttendDesc(int(heads), type, float(scale), int(window), int(sinks), int(max_rows), int(max_len))
 
 
@@ -693,6 +702,7 @@ def grinqh_attend_workspace_bytes(desc: KvDesc, heads: int, B: int, rows: int, m
     a = _attend_desc(desc, heads, GRINQH_BF16 if desc.format == GRINQH_KV_BF16 else GRINQH_F16, None, window, sinks,
                      max_rows, max_len)
     n = ctypes.c_size_t()
+    _fits(B, rows)
     _check(lib.grinqh_attend_workspace_bytes(ctypes.byref(desc), ctypes.byref(a), int(B), int(rows), ctypes.byref(n)))
     return int(n.value)
 
@@ -756,6 +766,7 @@ def _here(t, dtype, name, device, shape=None):
 def grinqh_kv_plan_workspace_bytes(B: int) -> int:
     """Workspace that grinqh_kv_plan needs for B sequences."""
     n = ctypes.c_size_t()
+    _fits(B)
     _check(lib.grinqh_kv_plan_workspace_bytes(int(B), ctypes.byref(n)))
     return int(n.value)
 
@@ -771,6 +782,7 @@ def grinqh_kv_plan(desc: KvDesc, pool: KvPool, batch: KvBatch, new_rows, rows: i
     if lens.dim() != 1 or table.dim() != 2:
         raise ValueError("seq_lens must have one axis and block_table two")
     (B, width), rows = table.shape, int(rows)
+    _fits(B, width, rows, free_pages.numel())
     i32, at = torch.int32, _current(free_pages)
     p = _KvPool(_here(free_pages, i32, "free_pages", at), _here(n_free, i32, "n_free", at, (1,)), free_pages.numel())
     if workspace is None:
@@ -819,6 +831,7 @@ def grinqh_norm(y=None, h=None, weight=None, bias=None, post_weight=None, post_b
     shape = (y if y is not None else h).shape
     if len(shape) != 2:
         raise ValueError(f"y and h must be [rows, n], got {tuple(shape)}")
+    _fits(*shape, pre, post)
     if h_out is None and y is not None:
         h_out = _empty(shape, (h if h is not None else y).dtype, first.device, stream)
     if x is None and pre != GRINQH_NORM_NONE:
