@@ -68,7 +68,10 @@ __device__ __forceinline__ const AttendArgs& late() {
 // 8 bits, whole call: 60 us, with workgroups of 8, 12 and 16 waves 59 .. 93; 32 sequences up to 8191 tokens 67 .. 75
 // and 75 .. 130 (over the numbers of parts).
 constexpr int rows_waves(int nb) { return nb == 1 ? 4 : 8; }
-constexpr int rows_per_simd(int format, int nb) { return nb == 1 && (format == GRINQH_KV_I8 || format == GRINQH_KV_I4) ? 3 : 2; }
+// 4-bit codes ask for more registers than three waves have (at 64 channels three stand there all the same): with three and 9 to
+// 13 registers in scratch, stored and read at the start and the end of a workgroup, one token over 131072 tokens took 43.7 us for
+// 40.1, 64 sequences of up to 2000 36.8 for 33.6; 200 of up to 700 in pages of 16 32.7 for 33.8.
+constexpr int rows_per_simd(int format, int nb) { return nb == 1 && format == GRINQH_KV_I8 ? 3 : 2; }
 
 // What is read for tokens that are not there, a block of 16 rows each: zeros behind the last token, NaN for K of a page
 // id out of range.  (A scale reads the first words.)
