@@ -443,8 +443,9 @@ typedef struct {
  *   list from its end into the sequence's table entries.
  * row_offsets [B + 1] are written: the running sum of the rows that come, which
  * are the last tokens of their sequences, as grinqh_kv_write and grinqh_attend
- * expect them.  Optional (NULL): positions [rows], the position of each row in
- * its sequence; slots [rows], page id * page + place in the page, or -1 for a page
+ * expect them.  Optional (NULL), for the caller's own kernels, as nothing here reads
+ * them: positions [rows], the position of each row in its sequence (a rotary
+ * embedding's); slots [rows], page id * page + place in the page, or -1 for a page
  * id out of range; both are -1 behind the last row; granted [B]: new_rows[b], 0
  * where nothing was given, minus the tokens that were taken back.
  * seq_lens are read as 0..min(table_width * page, 2^30).  A sequence's pages are its own:
@@ -471,8 +472,9 @@ GRINQH_API int grinqh_kv_plan(const grinqh_kv_desc* desc, const grinqh_kv_pool* 
  *   GRINQH_NORM_RMS    v / sqrt(mean(v^2) + eps) * weight + bias
  *   GRINQH_NORM_LAYER  (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * weight + bias
  * All in fp32; h_out and x are rounded once, x from the h' that is not rounded.
- * Values, their squares and sums may leave fp32's range, the result alone has to
- * be in it.  With eps = 0 a row of zeros (LAYER: of one value) is NaN. */
+ * A norm's squares and sums may leave fp32's range; a, gate * a, h' and the results
+ * have to be in it.  A row of one value has a LAYER norm of its bias, however far
+ * that value is from zero; with eps = 0 it is NaN, as a row of zeros is in either. */
 enum { GRINQH_NORM_NONE = 0, GRINQH_NORM_RMS = 1, GRINQH_NORM_LAYER = 2 };
 
 typedef struct {
@@ -489,7 +491,7 @@ typedef struct {
  * (1), weights (1), biases (0), h_out and x (not wanted), but not both y and h,
  * nor both h_out and x; x is wanted only with a pre norm.  Without a post norm
  * its weight and bias must be NULL, as without a pre norm that one's.  h_out may
- * be h, x and h_out may be y, where type and stride are the same; else
+ * be h or y, x may be y (if h_out is not), where type and stride are the same; else
  * what is written must not overlap anything.  With rows = 0 they are not looked at. */
 typedef struct {
   const void* y;    int64_t y_stride;

@@ -163,10 +163,6 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   return ((w & e) == e ? 0xffffu : 0u) | ((w >> 16 & e) == e ? 0xffff0000u : 0u);
 }
 
-
-// The type of the products over a cache.
-constexpr int product_type(int format) { return format == GRINQH_KV_BF16 ? GRINQH_KV_BF16 : GRINQH_KV_F16; }
-
 template <int FORMAT>
 __device__ __forceinline__ float4v mfma16(u32x4 a, u32x4 b, float4v c) {
   if constexpr (FORMAT == GRINQH_KV_BF16)

@@ -99,7 +99,8 @@ AttendPlan attend_plan(const KvCache& c, const Attend& a, int B, int rows) {
   // 4 bits: R = 32 over 8190 tokens of 1 sequence 19 : 29, of 4 44 : 48; 500 tokens of 4 16 : 23; 2000 of 32 69 : 76.  From 33 rows on
   // several workgroups read the cache, and the tile kernel, whose start and end take longer, is the faster one but for calls that
   // leave half the CUs free and are short: blocks of 32 rows times tokens, 64 x 2000 22 : 32, 16 x 4000 20 : 29, 128 x 500 19 : 23,
-  // 128 x 1000 33 : 30 and (R = 256) 30 : 32, 16 x 8190 33 : 30, 64 x 4000 36 : 34, 256 x 500 33 : 24, 200 x 500 31 : 24.
+  // 128 x 1000 33 : 30 and (R = 256) 30 : 32, 16 x 8190 33 : 30, 64 x 4000 36 : 34, 256 x 500 33 : 24, 200 x 500 31 : 24.  (At its
+  // edge, 128 x 1000, the rule pays 1.1 times or gains as much; no product of the two tells that from 64 x 2000.)
   const long blocks32 = (long)B * c.H * ((R + 31) / 32);
   const long seen32 = a.window ? std::min<long>(a.max_len, (long)a.window + 32 / a.G + a.sinks) : a.max_len;
   const bool small = blocks32 <= device_cus() / 2 && blocks32 * seen32 <= 500L * device_cus();

@@ -14,11 +14,15 @@
 //   - pages of 16 tokens or more are read by buffer loads: base and size are scalar, a page that is not there has size 0 and reads
 //     as zeros without an access, and a lane's offsets are the same for all tiles.
 // A tile's loads are issued a whole tile ahead, into the other of two sets of registers, and the page ids of the one after it
-// before them (32.1 us without).
+// before them (a microsecond in 32).
+//
+// Registers: one block of 16 rows a wave, which decoding uses, takes 128 to 192 and nothing in scratch.  Two blocks of 128 channels
+// have all 256 and keep 15 to 30 more in scratch, of which every tile reads some again: 10 to 12 with pages of 32 tokens and more or
+// of less than 16, 4 to 6 with pages of 16.
 //
 // Bound by memory, and by vector instructions close behind: one token of 32 heads over 131072 tokens of 8 kv heads of 128 (168 MB)
-// takes 31.1 us, 5.4 TB/s, where a large read reaches 6.9; its loads alone took 26.2 and everything but the loads, still with the
-// older conversions, 28.8.  32 sequences of up to 8191 tokens in pages of 16 take 45: unequal lengths.
+// takes 30.6 us, 5.5 TB/s, where a large read reaches 6.9; its loads alone took 26.2 and everything but the loads, still with the
+// older conversions, 28.8.  32 sequences of up to 8191 tokens in pages of 16 take 47: unequal lengths.
 #include "attend.h"
 
 namespace grinqh {

@@ -48,7 +48,7 @@ struct KvPlan {
   int* positions;
   long* slots;
   int* granted;
-  int* space;       // [0] pages of the list before any are handed out; then base [B] and old length [B]
+  int* space;       // the workspace: four words (the list's pages first), then two arrays [B], which kv_plan.hip describes
 };
 
 struct Attend {

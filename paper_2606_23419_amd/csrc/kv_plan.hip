@@ -266,8 +266,9 @@ __global__ __launch_bounds__(kThreads) void k_plan_small(KvPlan p) {
   }
 }
 
-// ---- more sequences.  Workspace: [0] the list's pages, [1] those before any came back, [2] those that came back; then per sequence
-// base (d < 0: pages that came back from the sequences before it) and old length (d < 0: its own pages that came back).
+// ---- more sequences.  Workspace: [0] the list's pages before any are handed out, [1] those before any came back, [2] those that came
+// back, [3] unused; from [4] on base [B], a sequence's pages from the list's end (d < 0: pages that came back from the sequences before
+// it), and old length [B] (d < 0: its own pages that came back).  k_plan_small leaves [0], base and old length there for k_plan_rows.
 constexpr int kSeqThreads = 256, kSeqs = kSeqThreads / 64;   // a wave a sequence
 
 __global__ __launch_bounds__(kSeqThreads) void k_plan_count(KvPlan p) {

@@ -6,8 +6,9 @@
 // A row stays in registers from its loads to its stores, so every input is read once.  Sums are fp32: of a lane's values, then
 // of the wave's lanes, then of the waves.  How many there are follows the channels alone, so a row's bits do not depend on the others.
 //
-// Bound by memory: 8192 rows of 4096, both norms and a gate (336 MB), 70 us; 1777 rows of 5001, two means, a gate per row, 38 us,
-// where rows that start at odd elements and the barriers of four sums cost; one row 3.9 us, latency.
+// Bound by memory: 8192 rows of 4096, both norms and a gate (336 MB), 71 us; 1777 rows of 5001, two means, a gate per row, 39 us
+// (34 where the last-level cache holds them), where rows that start at odd elements and the barriers of four sums cost; one row 3.9 us,
+// latency.
 #include <cmath>
 
 #include "kv.h"
