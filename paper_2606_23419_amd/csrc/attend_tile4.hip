@@ -15,7 +15,7 @@
 // At 64 channels a wave takes 195 to 208 registers; at 128 it has all 256, and 1 to 19 more in scratch (small pages and bf16 rows the
 // most), which are read at a workgroup's start and end and not in the tiles' loop: 4096 rows of bf16 take as long as of fp16.
 //
-// Bound by neither pipe alone.  4096 rows of 32 heads behind 32768 tokens (2.34 Tflop) take 2250 to 2330 us, 1000 to 1040 TFLOP/s;
+// Bound by neither pipe alone.  4096 rows of 32 heads behind 32768 tokens (2.34 Tflop) take 2250 to 2370 us, 990 to 1040 TFLOP/s;
 // the products' pipe is busy in 0.47 of the cycles and the vector one in 0.46, which are the same cycles in part only.  6 chunks
 // of 28 heads on 4 of 64 channels, window 2048: 67 to 70 us at the card's first clocks, which the next figures are of, 61 after 10 ms
 // of work; 1.44 us a tile of 64 tokens and 17 for the call of a few tiles.  What was
